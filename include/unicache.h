@@ -27,6 +27,11 @@
  *                        one launch (Sec. 3.1 and App. E)
  *   uc_plan_*            decode steps on a frozen, validated layout
  *                        (App. E "Cached metadata and execution plans")
+ *   uc_page_*            a cache held in 4 bits by pages: tables and slots
+ *                        from the sequences' lengths, rows in and out, and
+ *                        attention of ragged batches over it
+ *   uc_beam_*            beam search over such tables: the selection, and
+ *                        the reordering of tables and histories
  *   host helpers         byte accounting and budget -> policy configuration
  *                        (Sec. 3.3 Eq. 2 and Eq. 3, Sec. 3.4)
  *
@@ -582,6 +587,161 @@ uc_status uc_attend_batch(const uc_shape* shape, const uc_segment* const* segs,
 size_t uc_attend_batch_workspace_size(const uc_shape* shape,
                                       const uc_segment* const* segs,
                                       const int* n_segs, uc_dtype q_dt, int M);
+
+/* ------------------------------------------------------------------------ */
+/* Paged serving: the cache of one layer as pages of rows held in 4 bits, that
+ * sequences of any length share (App. E "Physical, type-aware KV storage" and
+ * "Batched attention and CFG execution": requests of different lengths in one
+ * launch).  The sequences' lengths live on the device, so a captured graph of
+ * the calls below serves every step.
+ *
+ * A page holds page_rows consecutive rows (tokens) of one sequence for every
+ * KV head; row j of sequence s lies in page table[s, j / page_rows], its slot
+ * is page * page_rows + j % page_rows.
+ *   codes_k, codes_v  [n_pages, Hkv, page_rows, D/2] bytes: two codes each,
+ *             the lower-numbered one in the low half.  Values' codes lie in
+ *             channel order; of keys, the 32-bit word (D/32) g + t of a row
+ *             holds channels 32 t + 8 g .. 32 t + 8 g + 7 (g < 4, t < D/32).
+ *   scale_k, scale_v  [n_pages, Hkv, page_rows, D/group] words: in the low
+ *             half the step s of a group of consecutive channels, in the high
+ *             half its minimum m, each a bf16.
+ * A code c stands for c * s + m, not rounded further.  A group x_1..x_G is
+ * quantised in IEEE binary32: m = bf16(min x); s = (max x - m) / 15 rounded up
+ * to 4 significant bits (so that c * s is a bf16 exactly); code = s > 0 ?
+ * clamp(rint((x - m) / s), 0, 15) : 0.  Before that every x is held to
+ * +-2^126 and a NaN becomes 0, so a cache written by uc_page_append holds
+ * finite values only.
+ * D is 64 or 128; group 32, 64 or 128 and at most D; page_rows a power of two
+ * in [16, 1024]; n_pages * page_rows < 2^31; pointers 16-byte aligned. */
+typedef struct {
+  int32_t n_pages, page_rows, Hkv, D, group, reserved;
+  uint8_t* codes_k;
+  uint8_t* codes_v;
+  uint32_t* scale_k;
+  uint32_t* scale_v;
+} uc_page_cache;
+
+/* The pages that no sequence holds: table [S, table_ld] and len [S] (int32,
+ * device) give each sequence the pages of its first ceil(len / page_rows)
+ * entries (at most table_ld; entries outside [0, n_pages) are passed over,
+ * pages may be named more than once).  free_list [n_pages] receives the
+ * others, ascending, -1 behind them, and pool [2] the pair (0, their count).
+ * A sequence ends by its len becoming 0.  ws: uc_page_free_workspace_size
+ * bytes. */
+uc_status uc_page_free(int S, int page_rows, int n_pages, const int32_t* table, int table_ld,
+                       const int32_t* len, int32_t* free_list, int32_t* pool, void* ws,
+                       size_t ws_bytes, void* stream);
+size_t uc_page_free_workspace_size(int n_pages);
+
+/* One step's tables and slots: sequence s, of len[s] rows, is to get
+ * new_len[s] more (negative counts as 0).  The sequences are served in order
+ * from the entries pool[0] .. pool[1] - 1 of free_list; s needs
+ * ceil((len + new) / page_rows) - ceil(len / page_rows) pages and is refused
+ * if the sum of needs up to it, its own included, exceeds the entries there
+ * are (unless it needs none), if its row of the table is too short, or if its
+ * tokens end beyond n_slots.
+ *   table    [S, table_ld] in and out: the new pages' entries are written
+ *   len_out  [S]   len + new, or len where refused
+ *   q_start  [S+1] sums of new_len: sequence s's tokens are q_start[s] ..
+ *            q_start[s+1] - 1 (held to n_slots), refused or not
+ *   slots    [n_slots] every token's slot; -1 for a refused sequence's and
+ *            behind the last token
+ *   pool_out [2] (entries taken up to, pool[1])
+ *   refused  [S] bytes: 1 where refused
+ * len_out may be len and pool_out may be pool; with others the call can be
+ * repeated and gives the same.  All int32 (refused uint8), device. */
+uc_status uc_page_step(int S, int page_rows, int n_pages, const int32_t* len, const int32_t* new_len,
+                       int32_t* table, int table_ld, const int32_t* free_list, const int32_t* pool,
+                       int32_t* len_out, int32_t* q_start, int32_t* slots, int n_slots,
+                       int32_t* pool_out, uint8_t* refused, void* stream);
+
+/* Quantises T tokens' rows into their slots: row h of token t is at
+ * k_new + t * ld + h * D (elements of dt, likewise v_new; ld >= Hkv * D, a
+ * multiple of 8, 4 for UC_F32; 16-byte aligned).  Slots outside the cache are
+ * passed over; no slot may occur twice.  copies, when n_copies > 0, is device
+ * int32 [n_copies, 3] as uc_beam_reorder writes it: rows 0 .. rows - 1 of page
+ * `from` are copied to page `to` (from < 0: nothing); the same call's slots
+ * must not lie in rows that are copied. */
+uc_status uc_page_append(const uc_page_cache* cache, const void* k_new, const void* v_new,
+                         uc_dtype dt, int64_t ld, int T, const int32_t* slots,
+                         const int32_t* copies, int n_copies, void* stream);
+
+/* The values held in T slots, as dense rows: k_out and v_out at t * ld + h * D
+ * in dt (alignment as for uc_page_append).  A slot outside the cache gives
+ * zeros. */
+uc_status uc_page_read(const uc_page_cache* cache, const int32_t* slots, int T, void* k_out,
+                       void* v_out, uc_dtype dt, int64_t ld, void* stream);
+
+/* Attention of a ragged batch over the cache, causal at the end of each
+ * sequence: with n = q_start[s+1] - q_start[s] query tokens and len = len[s]
+ * rows (the tokens' own, appended before, among them), query i < n sees rows
+ * j < len - n + i + 1 and
+ *   o = sum_j softmax_j(sm_scale * <q, k_j>) v_j ;
+ * a query that sees no row gets o = 0 and lse = -inf.
+ *   q       token t's head h at q + t * q_ld + h * D (q_dt; q_ld >= Hq * D, a
+ *           multiple of 8, 4 for UC_F32; 16-byte aligned)
+ *   o       [T, Hq, D] of q_dt, 16-byte aligned
+ *   lse     optional float [T, Hq]: natural-log log-sum-exp of the logits
+ *   max_q   at least the largest n; a sequence with more tokens may be left out
+ * Tokens of no sequence keep their o and lse.  q_start and len are held to
+ * [0, T] and the table's rows.  Rows of a sequence whose table names a page
+ * outside the cache within its length may be NaN, and those that see it are.
+ * Sequences with n * (Hq / Hkv) <= 16 and longer ones are taken by kernels of
+ * their own in the same call ("page_tokens", "page_prompt" for
+ * uc_last_kernel; UC_F32 queries and UC_PATH_VALU: "page_valu").  ws:
+ * uc_page_attend_workspace_size bytes; its size depends on the arguments
+ * alone, not on what the device holds. */
+uc_status uc_page_attend(const uc_page_cache* cache, int Hq, const void* q, uc_dtype q_dt,
+                         int64_t q_ld, int T, int S, int max_q, const int32_t* q_start,
+                         const int32_t* len, const int32_t* table, int table_ld, float sm_scale,
+                         void* o, float* lse, void* ws, size_t ws_bytes, void* stream);
+size_t uc_page_attend_workspace_size(const uc_page_cache* cache, int Hq, int T, int S, int max_q);
+
+/* ------------------------------------------------------------------------ */
+/* Beam search over paged sequences: R requests of W beams, beam b of request
+ * r being sequence r * W + b. */
+#define UC_MAX_BEAMS 32
+
+/* The W best continuations of every request.  logits [R*W, V] (dt, rows ld
+ * elements apart, ld >= V), score [R, W] float sums of log-probabilities.
+ * Continuation (b, v) has total score[b] + logit - lse, lse the natural-log
+ * log-sum-exp of the beam's logits; a beam with done[b] != 0 goes on by `pad`
+ * alone, at its score (done: optional uint8 [R, W]).  A total that is not
+ * finite counts as -inf (so does a NaN logit; a beam of score -inf, or whose
+ * logits hold +inf or nothing above -inf, has none above -inf).  The W largest
+ * totals are chosen, equal ones by the lower b * V + v:
+ *   score_out [R, W] float, descending; parent, token [R, W] int32;
+ *   done_out  optional uint8 [R, W]: done[parent], or token == eos
+ * score_out may be score and done_out may be done.  1 <= W <= UC_MAX_BEAMS,
+ * W <= V, W * V < 2^31, 0 <= pad < V; eos may be -1 (none).  Totals are
+ * formed in 64 bits from binary32 sums of exponentials.  ws:
+ * uc_beam_select_workspace_size bytes. */
+uc_status uc_beam_select(int R, int W, int V, const void* logits, uc_dtype dt, int64_t ld,
+                         const float* score, const uint8_t* done, int eos, int pad,
+                         float* score_out, int32_t* parent, int32_t* token, uint8_t* done_out,
+                         void* ws, size_t ws_bytes, void* stream);
+size_t uc_beam_select_workspace_size(int R, int W, int V);
+
+/* Moves the beams' tables and histories to their new places.  The beams of a
+ * request have one length, len[r * W], and each holds the page it is filling
+ * (entry len / page_rows when len % page_rows > 0) for itself alone; full
+ * pages may be shared.
+ *   table_out [R*W, table_ld]  row b: the entries of its parent that hold rows;
+ *             the page being filled stays with the first child of a beam, its
+ *             other children take over those of beams without children, the
+ *             first ones first.  Entries behind are not written.
+ *   copies    [R*W, 3]  (from, to, rows) of every beam whose page being filled
+ *             has to be copied by the next uc_page_append of every layer;
+ *             (-1, -1, 0) for the others
+ *   history   optional int32 [R*W, history_ld]: columns 0 .. n_history - 1 of
+ *             the parent go to history_out and token to column n_history
+ *             (n_history < history_ld)
+ * table_out may be table and history_out may be history.  parent is held to
+ * [0, W).  All int32, device. */
+uc_status uc_beam_reorder(int R, int W, const int32_t* parent, const int32_t* token,
+                          const int32_t* table, int table_ld, const int32_t* len, int page_rows,
+                          int32_t* table_out, int32_t* copies, const int32_t* history,
+                          int32_t* history_out, int64_t history_ld, int n_history, void* stream);
 
 /* ------------------------------------------------------------------------ */
 /* Dequantised rows of a packed segment (App. E storage; the stored-value

@@ -25,6 +25,7 @@ UC_F32, UC_F16, UC_BF16 = 0, 1, 2
 UC_SEG_DENSE, UC_SEG_PACKED = 0, 1
 UC_MAX_SEGMENTS = 8
 UC_PATH_AUTO, UC_PATH_VALU = 0, 1
+UC_MAX_BEAMS = 32
 
 TORCH_DT = {torch.float32: UC_F32, torch.float16: UC_F16, torch.bfloat16: UC_BF16}
 DT_TORCH = {v: k for k, v in TORCH_DT.items()}
@@ -54,6 +55,13 @@ class uc_segment(ctypes.Structure):
                 ("tail_v", ctypes.c_void_p)]
 
 
+class uc_page_cache(ctypes.Structure):
+    _fields_ = [("n_pages", ctypes.c_int32), ("page_rows", ctypes.c_int32), ("Hkv", ctypes.c_int32),
+                ("D", ctypes.c_int32), ("group", ctypes.c_int32), ("reserved", ctypes.c_int32),
+                ("codes_k", ctypes.c_void_p), ("codes_v", ctypes.c_void_p),
+                ("scale_k", ctypes.c_void_p), ("scale_v", ctypes.c_void_p)]
+
+
 class uc_budget_params(ctypes.Structure):
     _fields_ = [("Hq", ctypes.c_int32), ("Hkv", ctypes.c_int32), ("D", ctypes.c_int32),
                 ("M", ctypes.c_int32), ("n_segs", ctypes.c_int32), ("ev", ctypes.c_int32),
@@ -79,6 +87,7 @@ def _load():
     vp, i32, i64, u64, dbl, sz = (ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64,
                                   ctypes.c_uint64, ctypes.c_double, ctypes.c_size_t)
     shp, segp = ctypes.POINTER(uc_shape), ctypes.POINTER(uc_segment)
+    pcp = ctypes.POINTER(uc_page_cache)
     sigs = {
         "uc_score_importance": (i32, [shp, segp, i32, vp, i32, i32, ctypes.c_float, vp, vp, vp,
                                       sz, vp]),
@@ -129,6 +138,20 @@ def _load():
         "uc_plan_destroy": (i32, [vp]),
         "uc_plan_attend": (i32, [vp, vp, vp, vp, vp, vp, sz, vp]),
         "uc_plan_invalidate": (i32, [vp]),
+        "uc_page_free": (i32, [i32, i32, i32, vp, i32, vp, vp, vp, vp, sz, vp]),
+        "uc_page_free_workspace_size": (sz, [i32]),
+        "uc_page_step": (i32, [i32, i32, i32, vp, vp, vp, i32, vp, vp, vp, vp, vp, i32, vp, vp,
+                               vp]),
+        "uc_page_append": (i32, [pcp, vp, vp, i32, i64, i32, vp, vp, i32, vp]),
+        "uc_page_read": (i32, [pcp, vp, i32, vp, vp, i32, i64, vp]),
+        "uc_page_attend": (i32, [pcp, i32, vp, i32, i64, i32, i32, i32, vp, vp, vp, i32,
+                                 ctypes.c_float, vp, vp, vp, sz, vp]),
+        "uc_page_attend_workspace_size": (sz, [pcp, i32, i32, i32, i32]),
+        "uc_beam_select": (i32, [i32, i32, i32, vp, i32, i64, vp, vp, i32, i32, vp, vp, vp, vp, vp,
+                                 sz, vp]),
+        "uc_beam_select_workspace_size": (sz, [i32, i32, i32]),
+        "uc_beam_reorder": (i32, [i32, i32, vp, vp, vp, i32, vp, i32, vp, vp, vp, vp, i64, i32,
+                                  vp]),
         "uc_read_probe_unit": (sz, []),
         "uc_read_probe_sink_bytes": (sz, []),
         "uc_read_probe": (i32, [vp, sz, i32, vp, vp]),
@@ -494,6 +517,194 @@ def uc_attend_batch(shape: uc_shape, reqs: Sequence[Sequence[Segment]], q: torch
     _check(lib.uc_attend_batch(ctypes.byref(shape), ptrs, counts, q.data_ptr(), TORCH_DT[q.dtype],
                                M, ctypes.c_float(sm_scale), o.data_ptr(), _ptr(lse),
                                ws.data_ptr(), ws.numel(), _stream(stream)), "uc_attend_batch")
+
+
+class PageCache:
+    """The 4-bit pages of one layer (uc_page_cache) and the tensors they live
+    in: codes uint8 [n_pages, Hkv, page_rows, D/2], scale words int32
+    [n_pages, Hkv, page_rows, D/group]."""
+
+    def __init__(self, codes_k: torch.Tensor, codes_v: torch.Tensor, scale_k: torch.Tensor,
+                 scale_v: torch.Tensor):
+        n_pages, Hkv, P, half = codes_k.shape
+        for t, dt in ((codes_k, torch.uint8), (codes_v, torch.uint8), (scale_k, torch.int32),
+                      (scale_v, torch.int32)):
+            assert t.dtype == dt and t.is_contiguous() and t.device == codes_k.device
+        assert codes_v.shape == codes_k.shape and scale_v.shape == scale_k.shape
+        assert scale_k.shape[:3] == codes_k.shape[:3]
+        self.n_pages, self.Hkv, self.page_rows, self.D = n_pages, Hkv, P, 2 * half
+        self.group = self.D // scale_k.shape[3]
+        self.device = codes_k.device
+        self.t = {"codes_k": codes_k, "codes_v": codes_v, "scale_k": scale_k, "scale_v": scale_v}
+        self.desc = uc_page_cache(n_pages=n_pages, page_rows=P, Hkv=Hkv, D=self.D,
+                                  group=self.group, codes_k=codes_k.data_ptr(),
+                                  codes_v=codes_v.data_ptr(), scale_k=scale_k.data_ptr(),
+                                  scale_v=scale_v.data_ptr())
+        self._ref = ctypes.byref(self.desc)
+
+
+def page_cache(n_pages: int, page_rows: int, Hkv: int, D: int, group: int = 64,
+               device="cuda") -> PageCache:
+    """Allocate the pages of one layer (contents undefined until appended)."""
+    codes = [torch.empty(n_pages, Hkv, page_rows, D // 2, dtype=torch.uint8, device=device)
+             for _ in range(2)]
+    words = [torch.empty(n_pages, Hkv, page_rows, D // group, dtype=torch.int32, device=device)
+             for _ in range(2)]
+    return PageCache(*codes, *words)
+
+
+def _ints(*ts: Optional[torch.Tensor]):
+    """Device int32 tensors, contiguous, as the paged calls take them."""
+    for t in ts:
+        assert t is None or (t.dtype == torch.int32 and t.is_contiguous()), "int32, contiguous"
+    first = ts[0]
+    assert all(t is None or t.device == first.device for t in ts), "tensors on several devices"
+
+
+def _token_rows(x: torch.Tensor, heads: int, D: int) -> int:
+    """x [T, heads, D] with the heads of a token together; the distance of two
+    tokens in elements."""
+    assert x.dim() == 3 and x.shape[1] == heads and x.shape[2] == D, tuple(x.shape)
+    assert x.stride(2) == 1 and (heads == 1 or x.stride(1) == D), "a token's heads lie together"
+    return x.stride(0) if x.shape[0] > 1 else heads * D
+
+
+def uc_page_free(table: torch.Tensor, len: torch.Tensor, page_rows: int, free_list: torch.Tensor,
+                 pool: torch.Tensor, ws: Optional[torch.Tensor] = None, stream=None):
+    """The pages that no sequence of table [S, nb] / len [S] holds: free_list
+    [n_pages], pool [2] = (0, their count)."""
+    _ints(table, len, free_list, pool)
+    S, nb = table.shape
+    n_pages = free_list.numel()
+    assert len.numel() == S and pool.numel() == 2
+    if ws is None:
+        ws = _ws(lib.uc_page_free_workspace_size(n_pages), table.device)
+    _check(lib.uc_page_free(S, page_rows, n_pages, table.data_ptr(), nb, len.data_ptr(),
+                            free_list.data_ptr(), pool.data_ptr(), ws.data_ptr(), ws.numel(),
+                            _stream(stream)), "uc_page_free")
+
+
+def uc_page_step(len: torch.Tensor, new_len: torch.Tensor, table: torch.Tensor, page_rows: int,
+                 free_list: torch.Tensor, pool: torch.Tensor, len_out: torch.Tensor,
+                 q_start: torch.Tensor, slots: torch.Tensor, pool_out: torch.Tensor,
+                 refused: torch.Tensor, stream=None):
+    """One step's pages and slots: table [S, nb] gains the new pages' entries,
+    len_out [S], q_start [S + 1], slots [n_slots], pool_out [2] and refused
+    [S] (uint8) are written."""
+    _ints(table, len, new_len, free_list, pool, len_out, q_start, slots, pool_out)
+    S, nb = table.shape
+    assert len.numel() == new_len.numel() == len_out.numel() == refused.numel() == S
+    assert q_start.numel() == S + 1 and pool.numel() == pool_out.numel() == 2
+    assert refused.dtype == torch.uint8 and refused.is_contiguous()
+    _check(lib.uc_page_step(S, page_rows, free_list.numel(), len.data_ptr(), new_len.data_ptr(),
+                            table.data_ptr(), nb, free_list.data_ptr(), pool.data_ptr(),
+                            len_out.data_ptr(), q_start.data_ptr(), slots.data_ptr(),
+                            slots.numel(), pool_out.data_ptr(), refused.data_ptr(),
+                            _stream(stream)), "uc_page_step")
+
+
+def uc_page_append(cache: PageCache, k_new: torch.Tensor, v_new: torch.Tensor,
+                   slots: torch.Tensor, copies: Optional[torch.Tensor] = None, stream=None):
+    """Quantise k_new / v_new [T, Hkv, D] into slots [T]; copies [n, 3] as
+    uc_beam_reorder writes them."""
+    _ints(slots, copies)
+    T = slots.numel()
+    assert k_new.shape == v_new.shape and k_new.dtype == v_new.dtype and k_new.shape[0] == T
+    ld = _token_rows(k_new, cache.Hkv, cache.D)
+    assert _token_rows(v_new, cache.Hkv, cache.D) == ld, "k_new and v_new differ in their strides"
+    assert k_new.device == v_new.device == slots.device == cache.device
+    _check(lib.uc_page_append(cache._ref, k_new.data_ptr(), v_new.data_ptr(),
+                              TORCH_DT[k_new.dtype], ld, T, slots.data_ptr(), _ptr(copies),
+                              0 if copies is None else copies.numel() // 3, _stream(stream)),
+           "uc_page_append")
+
+
+def uc_page_read(cache: PageCache, slots: torch.Tensor, k_out: torch.Tensor, v_out: torch.Tensor,
+                 stream=None):
+    """The values held in slots [T] -> k_out / v_out [T, Hkv, D]."""
+    _ints(slots)
+    T = slots.numel()
+    assert k_out.shape == v_out.shape and k_out.dtype == v_out.dtype and k_out.shape[0] == T
+    ld = _token_rows(k_out, cache.Hkv, cache.D)
+    assert _token_rows(v_out, cache.Hkv, cache.D) == ld, "k_out and v_out differ in their strides"
+    assert k_out.device == v_out.device == slots.device == cache.device
+    _check(lib.uc_page_read(cache._ref, slots.data_ptr(), T, k_out.data_ptr(), v_out.data_ptr(),
+                            TORCH_DT[k_out.dtype], ld, _stream(stream)), "uc_page_read")
+
+
+def uc_page_attend_workspace_size(cache: PageCache, Hq: int, T: int, S: int, max_q: int) -> int:
+    return int(lib.uc_page_attend_workspace_size(cache._ref, Hq, T, S, max_q))
+
+
+def uc_page_attend(cache: PageCache, q: torch.Tensor, q_start: torch.Tensor, len: torch.Tensor,
+                   table: torch.Tensor, max_q: int, sm_scale: float, o: torch.Tensor,
+                   lse: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None,
+                   stream=None):
+    """Causal attention of the ragged tokens q [T, Hq, D] (sequence s: tokens
+    q_start[s] .. q_start[s + 1] - 1, the last ones of its len[s] rows) over
+    the cache's pages, into o [T, Hq, D] (q's dtype) and lse [T, Hq]."""
+    _ints(table, q_start, len)
+    S, nb = table.shape
+    T, Hq, D = q.shape
+    assert len.numel() == S and q_start.numel() == S + 1
+    assert o.shape == q.shape and o.dtype == q.dtype and o.is_contiguous()
+    assert lse is None or (lse.dtype == torch.float32 and lse.is_contiguous() and
+                           lse.numel() == T * Hq)
+    assert q.device == o.device == table.device == cache.device
+    ld = _token_rows(q, Hq, cache.D)
+    if ws is None:
+        ws = _ws(lib.uc_page_attend_workspace_size(cache._ref, Hq, T, S, max_q), q.device)
+    _check(lib.uc_page_attend(cache._ref, Hq, q.data_ptr(), TORCH_DT[q.dtype], ld, T, S, max_q,
+                              q_start.data_ptr(), len.data_ptr(), table.data_ptr(), nb, sm_scale,
+                              o.data_ptr(), _ptr(lse), ws.data_ptr(), ws.numel(),
+                              _stream(stream)), "uc_page_attend")
+    return o
+
+
+def uc_beam_select_workspace_size(R: int, W: int, V: int) -> int:
+    return int(lib.uc_beam_select_workspace_size(R, W, V))
+
+
+def uc_beam_select(logits: torch.Tensor, score: torch.Tensor, done: Optional[torch.Tensor],
+                   eos: int, pad: int, score_out: torch.Tensor, parent: torch.Tensor,
+                   token: torch.Tensor, done_out: Optional[torch.Tensor] = None,
+                   ws: Optional[torch.Tensor] = None, stream=None):
+    """The W best continuations of every request: logits [R, W, V] (rows at
+    one distance), score [R, W] float, done [R, W] uint8 or None."""
+    R, W, V = logits.shape
+    assert logits.stride(2) == 1 and (R == 1 or logits.stride(0) == W * logits.stride(1))
+    ld = logits.stride(1) if W > 1 else max(logits.stride(0) if R > 1 else V, V)
+    _ints(parent, token)
+    for t, dt in ((score, torch.float32), (score_out, torch.float32), (parent, torch.int32),
+                  (token, torch.int32), (done, torch.uint8), (done_out, torch.uint8)):
+        assert t is None or (t.dtype == dt and t.is_contiguous() and t.numel() == R * W and
+                             t.device == logits.device)
+    if ws is None:
+        ws = _ws(lib.uc_beam_select_workspace_size(R, W, V), logits.device)
+    _check(lib.uc_beam_select(R, W, V, logits.data_ptr(), TORCH_DT[logits.dtype], ld,
+                              score.data_ptr(), _ptr(done), eos, pad, score_out.data_ptr(),
+                              parent.data_ptr(), token.data_ptr(), _ptr(done_out), ws.data_ptr(),
+                              ws.numel(), _stream(stream)), "uc_beam_select")
+
+
+def uc_beam_reorder(parent: torch.Tensor, token: Optional[torch.Tensor], table: torch.Tensor,
+                    len: torch.Tensor, page_rows: int, table_out: torch.Tensor,
+                    copies: torch.Tensor, history: Optional[torch.Tensor] = None,
+                    history_out: Optional[torch.Tensor] = None, n_history: int = 0, stream=None):
+    """Moves tables [R * W, nb] (and histories [R * W, ld], of which n_history
+    columns are filled; token [R, W] joins them) to the beams' new places;
+    copies [R * W, 3] for the next uc_page_append of every layer."""
+    R, W = parent.shape
+    _ints(table, parent, token, len, table_out, copies, history, history_out)
+    assert table.shape[0] == R * W and table_out.shape == table.shape and len.numel() == R * W
+    assert copies.numel() == 3 * R * W and (token is None or token.numel() == R * W)
+    assert history is None or (history.shape[0] == R * W and history_out is not None and
+                               history_out.shape == history.shape and token is not None)
+    _check(lib.uc_beam_reorder(R, W, parent.data_ptr(), _ptr(token), table.data_ptr(),
+                               table.shape[1], len.data_ptr(), page_rows, table_out.data_ptr(),
+                               copies.data_ptr(), _ptr(history), _ptr(history_out),
+                               0 if history is None else history.shape[1], n_history,
+                               _stream(stream)), "uc_beam_reorder")
 
 
 def uc_dequantize_segment(shape: uc_shape, seg: Segment, k_out: torch.Tensor,

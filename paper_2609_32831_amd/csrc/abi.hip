@@ -86,23 +86,6 @@ struct TimerScope {
   }
 };
 
-uc_status fail(uc_status s, const char* fmt, ...) {
-  va_list ap;
-  va_start(ap, fmt);
-  vsnprintf(g_err, sizeof g_err, fmt, ap);
-  va_end(ap);
-  return s;
-}
-
-uc_status ok() {
-  g_err[0] = 0;
-  return UC_OK;
-}
-
-bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
-bool dtype_ok(int dt) { return dt == UC_F32 || dt == UC_F16 || dt == UC_BF16; }
-bool pow2(int x) { return x > 0 && (x & (x - 1)) == 0; }
-
 uc_status check_shape(const uc_shape* sh) {
   if (!sh) return fail(UC_E_INVALID, "shape is NULL");
   if (sh->B < 1 || sh->Hq < 1 || sh->Hkv < 1)
@@ -309,14 +292,30 @@ ChunkPlan score_col_plan(const uc_shape& sh, const KSegs& ks, int W) {
   return make_plan(ks, wide_path(sh, W) ? score_wide_chunk_rows() : 256, 1 << 30);
 }
 
+}  // namespace
+
+namespace uc {
+uc_status fail(uc_status s, const char* fmt, ...) {
+  va_list ap;
+  va_start(ap, fmt);
+  vsnprintf(g_err, sizeof g_err, fmt, ap);
+  va_end(ap);
+  return s;
+}
+
+uc_status ok() {
+  g_err[0] = 0;
+  return UC_OK;
+}
+
 uc_status launched(hipError_t e) {
   if (e != hipSuccess) return fail(UC_E_DEVICE, "HIP launch error: %s", hipGetErrorString(e));
   return ok();
 }
 
-}  // namespace
+void set_last_kernel(const char* name) { g_last_kernel = name; }
+int current_path() { return g_path.load(); }
 
-namespace uc {
 hipError_t kernel_timer_begin(hipStream_t st) {
   return g_ev_active[0] ? hipEventRecord(g_ev_active[0], st) : hipSuccess;
 }

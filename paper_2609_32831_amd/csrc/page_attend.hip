@@ -1,0 +1,626 @@
+// page_attend.hip -- attention over a paged cache held in 4 bits: single
+// tokens (at most 16 query rows of a KV head), prompts (any number), and the
+// vector-ALU form that stands for both.
+//
+// A sequence of len rows whose last n are this call's queries: query i sees
+// rows j < len - n + i + 1.  The n * G query rows of a KV head (G query heads
+// share it) are ordered r = i * G + g.
+//
+// Single tokens.  With code c, step s and minimum m of a group g of channels,
+//   q . k = sum_g s_g (q_g . c_g) + m_g sum(q_g)
+//   sum_j p_j v_jd = sum_j (p_j s_jg) c_jd + sum_j p_j m_jg
+// so the products run on whole codes, which a bf16 holds exactly, and the
+// steps are applied once per (key, group) instead of once per element.  The
+// codes become bf16 by two bit operations per pair: code | 0x4300 is 128 +
+// code; the 128s leave through the accumulators' start (keys: -128 sum(q_g))
+// and through the minima (values: m - 128 s).  Keys lie in operand order and
+// go from the load straight to the matrix instruction; values pass LDS still
+// as codes and are transposed by ds_read_b64_tr_b4 (16 x 16 codes).
+// Probabilities enter the second product as bf16 hi + lo parts (16 bits).
+//
+// Work is cut evenly without the host knowing any length: the tiles (64 keys)
+// of all sequences form one line, and workgroup w of W takes the w-th of W
+// equal pieces.  A sequence that lies within one piece is written by its
+// workgroup; one cut into several leaves a record (m, l, o) per piece, merged
+// by a second kernel in the order of the pieces.
+#include <algorithm>
+
+#include "page_common.h"
+
+namespace uc {
+namespace {
+
+using namespace mf;
+
+constexpr int WAVES = 4;
+constexpr int KT = 64;         // keys per tile
+constexpr float kLazy = 8.0f;  // base-2 headroom before the reference maximum is raised
+constexpr float kNone = -3.0e38f;  // the reference maximum before any visible key
+
+struct Seq {
+  int q0, n, len;
+};
+
+// a sequence's first token, tokens and rows, held to the call's arrays
+__device__ inline Seq seq_of(const PageAttendArgs& a, int s) {
+  Seq x;
+  x.q0 = min(max(a.q_start[s], 0), a.T);
+  x.n = min(max(a.q_start[s + 1], x.q0), a.T) - x.q0;
+  x.len = (int)min((int64_t)max(a.len[s], 0), min((int64_t)a.ld << a.pc.lgP, (int64_t)INT32_MAX));
+  return x;
+}
+
+template <int QT>
+__device__ inline float q_val(const void* q, int64_t i) {
+  return load_elem(q, QT, i);
+}
+
+template <int QT>
+__device__ inline void put(void* o, int64_t i, float x) {
+  if constexpr (QT == UC_F32) static_cast<float*>(o)[i] = x;
+  else static_cast<uint16_t*>(o)[i] = QT == UC_BF16 ? f32_to_bf16_bits(x) : f32_to_f16_bits(x);
+}
+
+// natural log-sum-exp of a row from its base-2 reference maximum and sum
+__device__ inline float lse_of(float m, float l) { return l > 0.0f ? (m + log2f(l)) * kLn2 : l == 0.0f ? -INFINITY : l; }
+
+// ---------------------------------------------------------------- vector ALU
+// One workgroup per (token, query head); keys in chunks of 256, one per
+// thread for the logits, one channel per thread for the values.
+template <int D, int QT>
+__global__ __launch_bounds__(256) void page_attend_valu_kernel(PageAttendArgs a) {
+  __shared__ float sq[D], sp[256], red[WAVES], so[256 / D][D];
+  __shared__ int64_t srow[256];
+  const int Hq = a.pc.Hkv * a.G, hq = blockIdx.x % Hq, t = blockIdx.x / Hq, h = hq / a.G;
+  // the sequence whose tokens include t
+  __shared__ int s_seq;
+  if (threadIdx.x == 0) s_seq = INT32_MAX;
+  __syncthreads();
+  for (int s = threadIdx.x; s < a.S; s += blockDim.x) {
+    const Seq x = seq_of(a, s);
+    if (t >= x.q0 && t < x.q0 + x.n) atomicMin(&s_seq, s);
+  }
+  __syncthreads();
+  if (s_seq == INT32_MAX) return;  // a row of no sequence stays as it was
+  const Seq x = seq_of(a, s_seq);
+  const int lim = max(0, min(x.len, (int)((int64_t)x.len - x.n + (t - x.q0) + 1)));
+  const int32_t* trow = a.table + (int64_t)s_seq * a.ld;
+  for (int d = threadIdx.x; d < D; d += blockDim.x) sq[d] = q_val<QT>(a.q, (int64_t)t * a.q_ld + hq * D + d);
+  const int ng = a.pc.ng, gsz = D / ng;
+  const int dim = threadIdx.x % D, part = threadIdx.x / D;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  float m = kNone, l = 0.0f, acc = 0.0f;
+  bool bad = false;
+  for (int j0 = 0; j0 < lim; j0 += 256) {
+    const int j = j0 + threadIdx.x;
+    float v = -INFINITY;
+    int64_t row = -1;
+    if (j < lim) {
+      const int page = page_of(trow, j, a.pc.lgP, a.pc.n_pages);
+      if (page < 0) bad = true;
+      else row = page_row(page, a.pc.Hkv, h, a.pc.lgP, j);
+    }
+    __syncthreads();  // sq is written; sp and srow are no longer read
+    if (row >= 0) {
+      float sum = 0.0f;
+      const uint32_t* codes = (const uint32_t*)a.pc.codes_k + row * (D / 8);
+      for (int w = 0; w < D / 8; ++w) {
+        const int c0 = 32 * (w % (D / 32)) + 8 * (w / (D / 32));  // first channel of the word
+        const uint32_t cw = codes[w], sw = a.pc.scale_k[row * ng + c0 / gsz];
+        for (int e = 0; e < 8; ++e)
+          sum = fmaf(sq[c0 + e], fmaf((float)((cw >> (4 * e)) & 15u), word_step(sw), word_min(sw)), sum);
+      }
+      v = sum * a.scale_log2;
+    }
+    srow[threadIdx.x] = row;
+    float mx = wave_max(v);
+    if (lane == 0) red[wave] = mx;
+    __syncthreads();
+    mx = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+    const float m_new = fmaxf(m, mx), alpha = exp2f(m - m_new);
+    m = m_new;
+    const float p = exp2f(v - m);
+    sp[threadIdx.x] = p;
+    l = l * alpha + p;  // this thread's keys
+    acc *= alpha;
+    __syncthreads();
+    const int n = min(256, lim - j0);
+    for (int i = part; i < n; i += 256 / D) {
+      if (srow[i] < 0) continue;
+      const uint8_t b = a.pc.codes_v[srow[i] * (D / 2) + dim / 2];
+      const uint32_t sw = a.pc.scale_v[srow[i] * ng + dim / gsz];
+      acc = fmaf(sp[i], fmaf((float)((b >> (4 * (dim & 1))) & 15), word_step(sw), word_min(sw)), acc);
+    }
+  }
+  __syncthreads();
+  so[part][dim] = acc;
+  l = wave_sum(l);
+  if (lane == 0) red[wave] = l;
+  const int any_bad = __syncthreads_or(bad);
+  l = (red[0] + red[1]) + (red[2] + red[3]);
+  if (any_bad) l = __builtin_nanf("");
+  if (threadIdx.x < D) {
+    float s = 0.0f;
+    for (int i = 0; i < 256 / D; ++i) s += so[i][threadIdx.x];
+    put<QT>(a.o, ((int64_t)t * Hq + hq) * D + threadIdx.x, l == 0.0f ? 0.0f : s / l);
+  }
+  if (threadIdx.x == 0 && a.lse) a.lse[(int64_t)t * Hq + hq] = lse_of(m, l);
+}
+
+// ---------------------------------------------------------------- the line of tiles
+// Pieces of the line: unit u of U belongs to piece (((u + 1) W - 1) / U).
+__device__ inline int64_t piece_first(int64_t U, int w, int W) { return U * w / W; }
+__device__ inline int piece_of(int64_t U, int64_t u, int W) { return (int)(((u + 1) * W - 1) / U); }
+
+// units of a sequence in the single-token kernel: its tiles, at least one so
+// that a row that sees nothing is written too; none where the prompt kernel
+// takes it
+__device__ inline int token_units(const Seq& x, int G) {
+  if (x.n == 0 || (int64_t)x.n * G > 16) return 0;
+  return max(1, (int)(((int64_t)x.len + KT - 1) / KT));
+}
+
+// a sequence cut into pieces first .. last; rows of the call it stands for
+struct Cut {
+  int seq, first, last, block;
+};
+
+// Records: piece w leaves at most two, [2 w] of a sequence it continues and
+// [2 w + 1] of one it begins; ROWS x (D + 2) floats: l, m, o.
+template <int D, int ROWS>
+__device__ inline float* record(float* rec, int w, int Hkv, int h, bool begins) {
+  return rec + (((int64_t)w * Hkv + h) * 2 + begins) * ROWS * (D + 2);
+}
+
+// ---------------------------------------------------------------- single tokens
+// codes of a word -> four pairs of bf16 (128 + code): pair i holds codes i
+// and i + 4
+__device__ inline u4 pairs(uint32_t w) {
+  const uint32_t m = 0x000F000Fu, k = 0x43004300u;
+  return u4{(w & m) | k, ((w >> 4) & m) | k, ((w >> 8) & m) | k, ((w >> 12) & m) | k};
+}
+
+template <int D>
+struct TileCodes {
+  static constexpr int VL = D / 32;  // 16-byte loads of a wave's share of values
+  uint32_t k[4][D / 32];             // four key blocks x the words of a lane
+  u4 v[VL];
+};
+
+template <int NG>
+struct TileWords {
+  uint32_t k[NG], v[NG];
+};
+
+template <int N>
+__device__ inline void load_words(const uint32_t* p, uint32_t (&w)[N]) {
+  if constexpr (N == 4) {
+    const u4 x = *reinterpret_cast<const u4*>(p);
+    w[0] = x[0], w[1] = x[1], w[2] = x[2], w[3] = x[3];
+  } else if constexpr (N == 2) {
+    const uint2 x = *reinterpret_cast<const uint2*>(p);
+    w[0] = x.x, w[1] = x.y;
+  } else {
+    w[0] = *p;
+  }
+}
+
+template <int D, int NG>
+struct WaveLds {
+  static constexpr int VROW = D / 2 + 8;  // bytes of a staged row of values
+  float k[2][NG][KT];                     // steps and minima of the tile's keys
+  float v[2][NG][KT];                     // steps and (minima - 128 steps) of its values
+  uint8_t codes[KT * VROW];
+};
+
+// D, NG: head dim and groups of a row; QP: bf16 parts of a query element
+template <int D, int NG, int QP>
+__global__ __launch_bounds__(256, 2) void page_tokens_kernel(PageAttendArgs a, int W_all, float* __restrict__ rec,
+                                                             Cut* __restrict__ cuts) {
+  constexpr int KS = D / 32;       // matrix steps over the channels
+  constexpr int DT = D / 16;       // tiles of 16 output channels
+  constexpr int GS = KS / NG > 0 ? KS / NG : 1;
+  constexpr int QT = QP == 1 ? UC_BF16 : UC_F16;
+  using Lds = WaveLds<D, NG>;
+  constexpr size_t kTiles = sizeof(Lds) * WAVES, kMerge = sizeof(float) * WAVES * 16 * (D + 2);
+  __shared__ __attribute__((aligned(16))) char lds[kTiles > kMerge ? kTiles : kMerge];
+  __shared__ int64_t s_units[256];
+  __shared__ int64_t s_part[WAVES];
+  __shared__ int s_bucket;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int i16 = lane & 15, g4 = lane >> 4;
+  const int Hkv = a.pc.Hkv, h = blockIdx.x % Hkv, w = blockIdx.x / Hkv;
+  const int G = a.G, Hq = G * Hkv, lgP = a.pc.lgP;
+
+  // this piece of the line: thread i counts sequences i c .. i c + c - 1
+  const int c = (a.S + 255) / 256;
+  int64_t mine = 0;
+  for (int s = threadIdx.x * c; s < min(a.S, (int)(threadIdx.x + 1) * c); ++s) mine += token_units(seq_of(a, s), G);
+  int64_t upto = mine;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int64_t y = __shfl_up(upto, o, 64);
+    if (lane >= o) upto += y;
+  }
+  if (lane == 63) s_part[wave] = upto;
+  __syncthreads();
+  int64_t U = 0;
+  for (int i = 0; i < WAVES; ++i) {
+    if (i < wave) upto += s_part[i];
+    U += s_part[i];
+  }
+  if (threadIdx.x == 0) cuts[blockIdx.x] = Cut{-1, 0, 0, 0};
+  if (U == 0) return;
+  // a tile per wave at least
+  const int W = (int)max((int64_t)1, min((int64_t)W_all, U / WAVES));
+  if (w >= W) return;
+  const int64_t u0 = piece_first(U, w, W), u1 = piece_first(U, w + 1, W);
+  s_units[threadIdx.x] = upto - mine;
+  if (upto - mine <= u0 && u0 < upto) s_bucket = threadIdx.x;
+  __syncthreads();
+  int s = s_bucket * c;
+  int64_t before = s_units[s_bucket];  // units before sequence s
+  Lds& L = *reinterpret_cast<Lds*>(lds + wave * sizeof(Lds));
+
+  for (int64_t u = u0; u < u1; ++s) {
+    const Seq x = seq_of(a, s);
+    const int units = token_units(x, G);
+    if (before + units <= u) {
+      before += units;
+      continue;
+    }
+    const int t0 = (int)(u - before), t1 = (int)min((int64_t)units, u1 - before);  // tiles [t0, t1) of sequence s
+    const int nq = x.n * G;
+    const int32_t* trow = a.table + (int64_t)s * a.ld;
+
+    // queries: the operand's channel order pairs codes i and i + 4
+    u4 qb[QP][KS];
+    float sq[NG];  // sum of the group's channels, all of them in every lane
+#pragma unroll
+    for (int g = 0; g < NG; ++g) sq[g] = 0.0f;
+    {
+      const int r = min(i16, nq - 1);
+      const int64_t base = (int64_t)(x.q0 + r / G) * a.q_ld + (int64_t)(h * G + r % G) * D + g4 * 8;
+#pragma unroll
+      for (int t = 0; t < KS; ++t) {
+        u4 raw = *reinterpret_cast<const u4*>(static_cast<const uint16_t*>(a.q) + base + t * 32);
+        if (i16 >= nq) raw = u4{0, 0, 0, 0};
+        float f[8];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          f[2 * e] = QP == 1 ? __uint_as_float(raw[e] << 16) : f16_to_f32((uint16_t)raw[e]);
+          f[2 * e + 1] = QP == 1 ? __uint_as_float(raw[e] & 0xFFFF0000u) : f16_to_f32((uint16_t)(raw[e] >> 16));
+          sq[t / GS] += f[2 * e] + f[2 * e + 1];
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const uint32_t hi = bf2(f[e], f[e + 4]);
+          qb[0][t][e] = hi;
+          if constexpr (QP == 2)
+            qb[1][t][e] = bf2(f[e] - __uint_as_float(hi << 16), f[e + 4] - __uint_as_float(hi & 0xFFFF0000u));
+        }
+      }
+#pragma unroll
+      for (int g = 0; g < NG; ++g) {
+        sq[g] += __shfl_xor(sq[g], 16, 64);
+        sq[g] += __shfl_xor(sq[g], 32, 64);
+      }
+    }
+    // first row that the lane's query does not see, and the least of them all
+    const int lim = max(0, min(x.len, (int)((int64_t)x.len - x.n + min(i16, nq - 1) / G + 1)));
+    const int lim_all = max(0, (int)((int64_t)x.len - x.n + 1));
+
+    float m = kNone, l = 0.0f, low[NG];
+    f4 acc[DT];
+#pragma unroll
+    for (int g = 0; g < NG; ++g) low[g] = 0.0f;
+#pragma unroll
+    for (int d = 0; d < DT; ++d) acc[d] = f4{0.f, 0.f, 0.f, 0.f};
+    bool bad = false;
+
+    if (x.len > 0) {
+      // pages of the lane's group of 16 keys (keys 16 g4 .. of the tile)
+      auto page_for = [&](int t) {
+        const int r = min(t * KT + g4 * 16, (x.len - 1) & ~15);
+        return page_of(trow, r, lgP, a.pc.n_pages);
+      };
+      TileCodes<D> tc;
+      TileWords<NG> tw;
+      auto issue = [&](int t, int page) {
+        if (t * KT + g4 * 16 < x.len && page < 0) bad = true;
+        page = max(page, 0);
+        const int r = min(t * KT + g4 * 16, (x.len - 1) & ~15);  // first row of the lane's group
+        const int64_t first = page_row(page, Hkv, h, lgP, r);      // its index in the cache
+        // keys: block b holds keys 16 (i16 / 4) + 4 b + i16 % 4, so that the
+        // product's rows 4 g4 .. + 3 of the four blocks are keys 16 g4 .. + 15
+        const int64_t kf = __shfl(first, (i16 >> 2) * 16, 64) + (i16 & 3);
+        const uint32_t* kc = (const uint32_t*)a.pc.codes_k + kf * (D / 8) + g4 * KS;
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+          if constexpr (KS == 4) {
+            const u4 x4 = *reinterpret_cast<const u4*>(kc + b * 4 * (D / 8));
+            tc.k[b][0] = x4[0], tc.k[b][1] = x4[1], tc.k[b][2] = x4[2], tc.k[b][3] = x4[3];
+          } else {
+            const uint2 x2 = *reinterpret_cast<const uint2*>(kc + b * 4 * (D / 8));
+            tc.k[b][0] = x2.x, tc.k[b][1] = x2.y;
+          }
+        }
+        // values: load i covers 64 / VL keys, whole rows
+        constexpr int CH = D / 32;  // 16-byte chunks of a row
+#pragma unroll
+        for (int i = 0; i < TileCodes<D>::VL; ++i) {
+          const int key = i * (KT / TileCodes<D>::VL) + lane / CH;
+          const int64_t vf = __shfl(first, (key >> 4) * 16, 64) + (key & 15);
+          tc.v[i] = *reinterpret_cast<const u4*>(a.pc.codes_v + vf * (D / 2) + (lane % CH) * 16);
+        }
+        load_words<NG>(a.pc.scale_k + (first + i16) * NG, tw.k);
+        load_words<NG>(a.pc.scale_v + (first + i16) * NG, tw.v);
+        if (t * KT + lane >= x.len) {  // rows behind the sequence hold anything
+#pragma unroll
+          for (int g = 0; g < NG; ++g) tw.k[g] = tw.v[g] = 0;
+        }
+      };
+
+      int t = t0 + wave;
+      if (t < t1) issue(t, page_for(t));
+      for (; t < t1; t += WAVES) {
+        // stage the tile: values as codes, words as floats
+        constexpr int CH = D / 32;
+#pragma unroll
+        for (int i = 0; i < TileCodes<D>::VL; ++i) {
+          const int key = i * (KT / TileCodes<D>::VL) + lane / CH;
+          uint2* dst = reinterpret_cast<uint2*>(L.codes + key * Lds::VROW + (lane % CH) * 16);
+          dst[0] = uint2{tc.v[i][0], tc.v[i][1]};
+          dst[1] = uint2{tc.v[i][2], tc.v[i][3]};
+        }
+#pragma unroll
+        for (int g = 0; g < NG; ++g) {
+          L.k[0][g][lane] = word_step(tw.k[g]);
+          L.k[1][g][lane] = word_min(tw.k[g]);
+          const float sv = word_step(tw.v[g]);
+          L.v[0][g][lane] = sv;
+          L.v[1][g][lane] = fmaf(-128.0f, sv, word_min(tw.v[g]));
+        }
+        __builtin_amdgcn_wave_barrier();
+
+        // logits: p[b][j] of key 16 g4 + 4 b + j
+        float p[16];
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+          f4 sum = f4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int g = 0; g < NG; ++g) {
+            const float z = -128.0f * sq[g];
+            f4 dot = f4{z, z, z, z};
+#pragma unroll
+            for (int t2 = g * GS; t2 < (g + 1) * GS; ++t2) {
+              const u4 kb = pairs(tc.k[b][t2]);
+#pragma unroll
+              for (int qp = 0; qp < QP; ++qp) dot = mfma(kb, qb[qp][t2], dot);
+            }
+            const f4 st = *reinterpret_cast<const f4*>(&L.k[0][g][g4 * 16 + b * 4]);
+            const f4 mn = *reinterpret_cast<const f4*>(&L.k[1][g][g4 * 16 + b * 4]);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) sum[j] = fmaf(st[j], dot[j], fmaf(mn[j], sq[g], sum[j]));
+          }
+#pragma unroll
+          for (int j = 0; j < 4; ++j) p[b * 4 + j] = sum[j];
+        }
+        const int r0 = t * KT;
+        if (r0 + KT > lim_all) {
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            if (r0 + g4 * 16 + e >= lim) p[e] = -INFINITY;
+        }
+        // the next tile's loads: the codes of this one's keys are used up
+        const int tn = t + WAVES;
+        if (tn < t1) issue(tn, page_for(tn));
+
+        // softmax against a lazily raised reference maximum
+        float mx = p[0];
+#pragma unroll
+        for (int e = 1; e < 16; ++e) mx = fmaxf(mx, p[e]);
+        mx *= a.scale_log2;
+        if (__builtin_amdgcn_ballot_w64(mx > m + kLazy)) {
+          mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+          mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+          const float m_new = fmaxf(m, mx), alpha = __builtin_amdgcn_exp2f(m - m_new);
+          m = m_new;
+          l *= alpha;
+#pragma unroll
+          for (int g = 0; g < NG; ++g) low[g] *= alpha;
+#pragma unroll
+          for (int d = 0; d < DT; ++d) acc[d] *= alpha;
+        }
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          p[e] = __builtin_amdgcn_exp2f(fmaf(p[e], a.scale_log2, -m));
+          l += p[e];
+        }
+        // O^T += V^T P, group by group
+#pragma unroll
+        for (int g = 0; g < NG; ++g) {
+          float e1[8], e2[8];  // (key i, key i + 4) pairs of keys 0 .. 7 and 8 .. 15
+#pragma unroll
+          for (int b = 0; b < 4; ++b) {
+            const f4 st = *reinterpret_cast<const f4*>(&L.v[0][g][g4 * 16 + b * 4]);
+            const f4 mn = *reinterpret_cast<const f4*>(&L.v[1][g][g4 * 16 + b * 4]);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const float ps = p[b * 4 + j] * st[j];
+              (b < 2 ? e1 : e2)[2 * j + (b & 1)] = ps;
+              low[g] = fmaf(p[b * 4 + j], mn[j], low[g]);
+            }
+          }
+          u4 h1, l1, h2, l2;
+          split_p(e1, h1, l1);
+          split_p(e2, h2, l2);
+#pragma unroll
+          for (int d = g * (DT / NG); d < (g + 1) * (DT / NG); ++d) {
+            typedef int v2i __attribute__((ext_vector_type(2)));
+            typedef __attribute__((address_space(3))) v2i lds_v2i;
+            const v2i cw = __builtin_amdgcn_ds_read_tr4_b64_v2i32(
+                (lds_v2i*)(L.codes + (g4 * 16 + i16) * Lds::VROW + d * 8));
+            const u4 va = pairs((uint32_t)cw[0]), vb = pairs((uint32_t)cw[1]);
+            acc[d] = mfma(va, h1, acc[d]);
+            acc[d] = mfma(va, l1, acc[d]);
+            acc[d] = mfma(vb, h2, acc[d]);
+            acc[d] = mfma(vb, l2, acc[d]);
+          }
+        }
+        __builtin_amdgcn_wave_barrier();  // the tile's LDS is written again
+      }
+    }
+
+    // merge the waves
+    l += __shfl_xor(l, 16, 64);
+    l += __shfl_xor(l, 32, 64);
+#pragma unroll
+    for (int g = 0; g < NG; ++g) {
+      low[g] += __shfl_xor(low[g], 16, 64);
+      low[g] += __shfl_xor(low[g], 32, 64);
+    }
+    const int any_bad = __syncthreads_or(bad);
+    float* mo = reinterpret_cast<float*>(lds);  // [WAVES][16][D]
+    float* ml = mo + WAVES * 16 * D;            // [WAVES][16] m, then l
+    if (g4 == 0) {
+      ml[wave * 16 + i16] = m;
+      ml[WAVES * 16 + wave * 16 + i16] = l;
+    }
+#pragma unroll
+    for (int d = 0; d < DT; ++d) {
+      f4 y = acc[d];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) y[j] += low[d / (DT / NG)];
+      *reinterpret_cast<f4*>(&mo[(wave * 16 + i16) * D + d * 16 + g4 * 4]) = y;
+    }
+    __syncthreads();
+    const bool begins = before >= u0, ends = before + units <= u1;
+    float* out = record<D, 16>(rec, w, Hkv, h, begins);
+    for (int e = threadIdx.x; e < nq * D; e += blockDim.x) {
+      const int r = e / D, d = e % D;
+      float M = kNone, wt[WAVES], ls = 0.0f, y = 0.0f;
+#pragma unroll
+      for (int i = 0; i < WAVES; ++i) M = fmaxf(M, ml[i * 16 + r]);
+#pragma unroll
+      for (int i = 0; i < WAVES; ++i) {
+        wt[i] = exp2f(ml[i * 16 + r] - M);
+        ls = fmaf(wt[i], ml[WAVES * 16 + i * 16 + r], ls);
+        y = fmaf(wt[i], mo[(i * 16 + r) * D + d], y);
+      }
+      if (any_bad) ls = __builtin_nanf("");
+      if (begins && ends) {
+        const int64_t at = (int64_t)(x.q0 + r / G) * Hq + h * G + r % G;
+        put<QT>(a.o, at * D + d, ls == 0.0f ? 0.0f : y / ls);
+        if (d == 0 && a.lse) a.lse[at] = lse_of(M, ls);
+      } else {
+        out[r * (D + 2) + 2 + d] = y;
+        if (d == 0) {
+          out[r * (D + 2)] = M;
+          out[r * (D + 2) + 1] = ls;
+        }
+      }
+    }
+    if (begins && !ends && threadIdx.x == 0)
+      cuts[blockIdx.x] = Cut{s, w, piece_of(U, before + units - 1, W), 0};
+    __syncthreads();  // LDS is written again
+    before += units;
+    u = before;
+  }
+}
+
+// one workgroup per cut: its pieces' records in order, ROWS query rows from
+// row `block` of the sequence on
+template <int D, int ROWS, int QT>
+__global__ __launch_bounds__(256) void page_merge_kernel(PageAttendArgs a, const float* __restrict__ rec,
+                                                         const Cut* __restrict__ cuts) {
+  const Cut k = cuts[blockIdx.x];
+  if (k.seq < 0) return;
+  const int Hkv = a.pc.Hkv, h = blockIdx.x % Hkv, G = a.G, Hq = G * Hkv;
+  const Seq x = seq_of(a, k.seq);
+  const int rows = (int)min((int64_t)ROWS, (int64_t)x.n * G - k.block);
+  for (int e = blockIdx.y * blockDim.x + threadIdx.x; e < rows * D; e += gridDim.y * blockDim.x) {
+    const int r = e / D, d = e % D;
+    float M = kNone, l = 0.0f, y = 0.0f;
+    for (int w = k.first; w <= k.last; ++w) {
+      const float* p = rec + (((int64_t)w * Hkv + h) * 2 + (w == k.first)) * ROWS * (D + 2) + r * (D + 2);
+      const float m_new = fmaxf(M, p[0]), old = exp2f(M - m_new), add = exp2f(p[0] - m_new);
+      l = l * old + p[1] * add;
+      y = y * old + p[2 + d] * add;
+      M = m_new;
+    }
+    const int i = (k.block + r) / G, g = (k.block + r) % G;
+    const int64_t at = (int64_t)(x.q0 + i) * Hq + h * G + g;
+    put<QT>(a.o, at * D + d, l == 0.0f ? 0.0f : y / l);
+    if (d == 0 && a.lse) a.lse[at] = lse_of(M, l);
+  }
+}
+
+}  // namespace
+
+// pieces of the line per KV head: two workgroups per CU in one round
+static int token_pieces(const PageCache& pc, int S, int ld) {
+  const int64_t most = (int64_t)S * std::max<int64_t>(1, (((int64_t)ld << pc.lgP) + KT - 1) / KT) / WAVES;
+  return (int)std::max<int64_t>(1, std::min<int64_t>(std::max(1, 2 * device_cus() / pc.Hkv), most));
+}
+
+size_t page_tokens_workspace(const PageCache& pc) {
+  const size_t W = std::max(1, 2 * device_cus() / pc.Hkv) * (size_t)pc.Hkv;
+  return ((W * sizeof(Cut) + 255) & ~(size_t)255) + W * 2 * 16 * (pc.D + 2) * sizeof(float);
+}
+
+hipError_t launch_page_tokens(const PageAttendArgs& a, int q_dt, void* ws, hipStream_t st) {
+  const int W = token_pieces(a.pc, a.S, a.ld), n = W * a.pc.Hkv;
+  Cut* cuts = (Cut*)ws;
+  float* rec = (float*)((char*)ws + (((size_t)n * sizeof(Cut) + 255) & ~(size_t)255));
+#define UC_TOKENS(DIM, NGR)                                                                                \
+  {                                                                                                        \
+    if (q_dt == UC_BF16) {                                                                                 \
+      hipLaunchKernelGGL((page_tokens_kernel<DIM, NGR, 1>), dim3(n), dim3(256), 0, st, a, W, rec, cuts);   \
+      hipLaunchKernelGGL((page_merge_kernel<DIM, 16, UC_BF16>), dim3(n, 2), dim3(256), 0, st, a, rec, cuts); \
+    } else {                                                                                               \
+      hipLaunchKernelGGL((page_tokens_kernel<DIM, NGR, 2>), dim3(n), dim3(256), 0, st, a, W, rec, cuts);   \
+      hipLaunchKernelGGL((page_merge_kernel<DIM, 16, UC_F16>), dim3(n, 2), dim3(256), 0, st, a, rec, cuts);  \
+    }                                                                                                      \
+  }
+  if (a.pc.D == 128) {
+    if (a.pc.ng == 4) UC_TOKENS(128, 4)
+    else if (a.pc.ng == 2) UC_TOKENS(128, 2)
+    else UC_TOKENS(128, 1)
+  } else {
+    if (a.pc.ng == 2) UC_TOKENS(64, 2)
+    else UC_TOKENS(64, 1)
+  }
+#undef UC_TOKENS
+  return hipGetLastError();
+}
+
+hipError_t launch_page_valu(const PageAttendArgs& a, int q_dt, hipStream_t st) {
+  const dim3 grid((uint32_t)((int64_t)a.T * a.pc.Hkv * a.G));
+#define UC_VALU(DIM, TYPE) \
+  hipLaunchKernelGGL((page_attend_valu_kernel<DIM, TYPE>), grid, dim3(256), 0, st, a)
+  if (a.pc.D == 128) {
+    if (q_dt == UC_BF16) UC_VALU(128, UC_BF16);
+    else if (q_dt == UC_F16) UC_VALU(128, UC_F16);
+    else UC_VALU(128, UC_F32);
+  } else {
+    if (q_dt == UC_BF16) UC_VALU(64, UC_BF16);
+    else if (q_dt == UC_F16) UC_VALU(64, UC_F16);
+    else UC_VALU(64, UC_F32);
+  }
+#undef UC_VALU
+  return hipGetLastError();
+}
+
+size_t page_attend_workspace(const PageCache& pc, int G, int T, int S, int max_q) { return page_tokens_workspace(pc); }
+
+hipError_t launch_page_attend(const PageAttendArgs& a, int q_dt, int max_q, bool valu, void* ws, hipStream_t st) {
+  if (valu || (int64_t)max_q * a.G > 16) {
+    set_last_kernel("page_valu");
+    return launch_page_valu(a, q_dt, st);
+  }
+  set_last_kernel("page_tokens");
+  return launch_page_tokens(a, q_dt, ws, st);
+}
+
+}  // namespace uc

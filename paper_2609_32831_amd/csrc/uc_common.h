@@ -174,6 +174,18 @@ constexpr double kLn2d = 0.6931471805599453;
 
 }  // namespace uc
 
+// ---- error reporting and state of the C entry points (abi.hip) ---------------
+namespace uc {
+uc_status fail(uc_status s, const char* fmt, ...);  // sets uc_last_error()
+uc_status ok();
+uc_status launched(hipError_t e);
+void set_last_kernel(const char* name);
+int current_path();
+inline bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
+inline bool dtype_ok(int dt) { return dt == UC_F32 || dt == UC_F16 || dt == UC_BF16; }
+inline bool pow2(int x) { return x > 0 && (x & (x - 1)) == 0; }
+}  // namespace uc
+
 // ---- launchers implemented in the kernel translation units -------------------
 namespace uc {
 // Events bracketing the attention kernel of the current uc_attend_mixed call

@@ -1,0 +1,581 @@
+"""GPU parity of the paged 4-bit cache and of beam search over it
+(``uc_page_*``, ``uc_beam_*``) against a plain reference in 64 bits.
+
+Tolerances.  Codes, words, tables, slots, copies and beams: equal.  Values
+read back: one rounding, half a step of the type (eps / 2 relative, bf16 2^-8,
+fp16 2^-11).  Attention: the repository's bar for attention outputs (2e-3
+absolute, 1e-3 of the norm) plus that one rounding of the output; the
+normaliser as in the other attention tests (1e-4 and 1e-5 relative)."""
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+if not torch.cuda.is_available():
+    pytest.skip("needs a GPU", allow_module_level=True)
+
+import paged_ref as ref  # noqa: E402
+import paper_2609_32831_amd as uc  # noqa: E402
+
+DT = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
+
+
+def _case(**kw):
+    print("CASE", " ".join(f"{k}={v}" for k, v in kw.items()), flush=True)
+
+
+def half(dtype):
+    return torch.finfo(DT[dtype]).eps / 2
+
+
+def i32(x):
+    return torch.tensor(np.asarray(x), dtype=torch.int32, device="cuda")
+
+
+def f64(t):
+    return t.double().cpu().numpy()
+
+
+def make_cache(lens, P, Hkv, D, group, seed, spare=2, scale=1.0, outlier=True):
+    """A host cache with lens rows of random content behind a random table."""
+    r = np.random.default_rng(seed)
+    count = [-(-n // P) for n in lens]
+    n_pages = sum(count) + spare
+    order = r.permutation(n_pages)
+    nb = max(count + [1])
+    table = np.full((len(lens), nb), -1, np.int64)
+    at = 0
+    for s, c in enumerate(count):
+        table[s, :c] = order[at:at + c]
+        at += c
+    cache = ref.Cache(n_pages, P, Hkv, D, group, seed)
+    for s, n in enumerate(lens):
+        if n == 0:
+            continue
+        k = (r.standard_normal((n, Hkv, D)) * scale).astype(np.float32)
+        if outlier:
+            k[:, :, 5] *= 8
+        v = (r.standard_normal((n, Hkv, D)) * scale).astype(np.float32)
+        sl = ref.slots_of(table[s], n, P)
+        order_k = ref.key_order(D)
+        (qk, wk), (qv, wv) = ref.quantise(k, group), ref.quantise(v, group)
+        p, i = sl // P, sl % P
+        cache.ck[p, :, i], cache.cv[p, :, i] = ref.pack(qk[..., order_k]), ref.pack(qv)
+        cache.sk[p, :, i], cache.sv[p, :, i] = wk, wv
+    return cache, table
+
+
+# ---------------------------------------------------------------- rows
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("D,group,P,Hkv,T", [(128, 32, 16, 4, 37), (128, 64, 64, 1, 1), (128, 128, 256, 3, 130),
+                                             (64, 32, 32, 2, 65), (64, 64, 16, 5, 300)])
+def test_rows_in_and_out(dtype, D, group, P, Hkv, T):
+    _case(test="rows", dtype=dtype, D=D, group=group, P=P, Hkv=Hkv, T=T)
+    r = np.random.default_rng(T)
+    n_pages = -(-T // P) + 2
+    host = ref.Cache(n_pages, P, Hkv, D, group, 3)
+    cache = host.device(uc)
+    # the rows as a slice of a fused projection: tokens further apart than their heads are wide
+    wide = torch.tensor(r.standard_normal((T, 3 * Hkv + 1, D)) * 3, device="cuda").to(DT[dtype])
+    k, v = wide[:, Hkv:2 * Hkv], wide[:, 2 * Hkv:3 * Hkv]
+    k[:, :, 5 % D] *= 8
+    slots = r.permutation(n_pages * P)[:T]
+    slots[T // 2] = -1 if T > 1 else slots[0]
+    if T > 3:
+        slots[2] = n_pages * P + 7  # outside: passed over
+    uc.uc_page_append(cache, k, v, i32(slots))
+    host.append(k.float().cpu().numpy(), v.float().cpu().numpy(), slots)
+    for name, want in (("codes_k", host.ck), ("codes_v", host.cv), ("scale_k", host.sk), ("scale_v", host.sv)):
+        got = cache.t[name].cpu().numpy()
+        assert np.array_equal(got.view(np.uint8), want.view(np.uint8)), name
+    out = torch.full((2, T, Hkv + 1, D), 7.0, device="cuda").to(DT[dtype])
+    uc.uc_page_read(cache, i32(slots), out[0, :, :Hkv], out[1, :, :Hkv])
+    live = (slots >= 0) & (slots < n_pages * P)
+    for got, want in zip(out, host.rows(np.where(live, slots, 0))):
+        want = np.where(live[:, None, None], want, 0)
+        assert np.all(np.abs(f64(got[:, :Hkv]) - want) <= half(dtype) * np.abs(want) + 1e-30)
+        assert torch.all(got[:, Hkv:] == 7.0)
+
+
+def test_rows_of_special_values():
+    D, group, P = 128, 32, 16
+    x = np.zeros((8, 1, D), np.float32)
+    x[1] = 3.25
+    x[2, 0, ::2] = np.inf
+    x[2, 0, 1] = -np.inf
+    x[3, 0, ::3] = np.nan
+    x[4] = np.linspace(-3e38, 3e38, D)
+    x[5] = np.linspace(0, 1e-42, D)
+    x[6] = np.linspace(1000, 1000.1, D)
+    x[7] = -np.linspace(0, 1, D) ** 9
+    host = ref.Cache(1, P, 1, D, group, 1)
+    cache = host.device(uc)
+    t = torch.from_numpy(x).cuda()
+    uc.uc_page_append(cache, t, t, i32(range(8)))
+    with np.errstate(over="ignore"):
+        host.append(x, x, range(8))
+    assert np.array_equal(cache.t["codes_k"].cpu().numpy(), host.ck)
+    assert np.array_equal(cache.t["codes_v"].cpu().numpy(), host.cv)
+    assert np.array_equal(cache.t["scale_k"].cpu().numpy().view(np.uint32), host.sk)
+    assert np.all(np.isfinite(host.rows(range(8))[0]))  # what a mask hides cannot spread
+
+
+def test_copies_join_the_append():
+    D, group, P, Hkv = 64, 32, 16, 2
+    host = ref.Cache(6, P, Hkv, D, group, 5)
+    cache = host.device(uc)
+    copies = np.array([[0, 3, 5], [-1, -1, 0], [1, 4, 16], [2, 9, 4], [2, 2, 4]])
+    k = torch.randn(2, Hkv, D, device="cuda", dtype=torch.bfloat16)
+    slots = [3 * P + 5, 0 * P + 5]
+    uc.uc_page_append(cache, k, k, i32(slots), i32(copies))
+    host.copy(copies[[0, 2]])
+    host.append(k.float().cpu().numpy(), k.float().cpu().numpy(), slots)
+    for name, want in (("codes_k", host.ck), ("codes_v", host.cv), ("scale_k", host.sk), ("scale_v", host.sv)):
+        assert np.array_equal(cache.t[name].cpu().numpy().view(np.uint8), want.view(np.uint8)), name
+    # copies alone
+    uc.uc_page_append(cache, k[:0], k[:0], i32(np.zeros(0)), i32([[1, 0, 16]]))
+    host.copy([[1, 0, 16]])
+    assert np.array_equal(cache.t["codes_v"].cpu().numpy(), host.cv)
+
+
+# ---------------------------------------------------------------- tables
+
+TABLES = [  # S, P, most rows, most new, free pages to spare, table columns to spare, slots to spare
+    (1, 16, 0, 1, 1, 0, 0), (5, 16, 40, 3, 50, 1, 4), (70, 64, 900, 300, 400, 2, 0), (300, 32, 500, 40, 200, 0, 9),
+    (1500, 16, 90, 2, 100, 1, 3), (33, 256, 5000, 700, 9, 0, -50), (9, 16, 30000, 20000, 5000, 0, 1),
+]
+
+
+@pytest.mark.parametrize("S,P,most,new,spare,wide,extra", TABLES)
+def test_tables_and_slots(S, P, most, new, spare, wide, extra):
+    _case(test="tables", S=S, P=P, most=most, new=new)
+    r = np.random.default_rng(S + P)
+    lens = r.integers(0, most + 1, S)
+    lens[r.random(S) < 0.2] = 0
+    more = np.where(r.random(S) < 0.7, 1, r.integers(-2, new + 1, S))
+    count = -(-lens // P)
+    n_pages = int(count.sum()) + spare
+    nb = int(max(-(-(lens + np.maximum(more, 0)) // P))) + wide
+    nb = max(nb - (S == 33), 1)  # a row too short for the longest
+    table = np.full((S, nb), -7, np.int64)
+    order = r.permutation(n_pages)
+    at = 0
+    for s in range(S):
+        c = min(int(count[s]), nb)
+        table[s, :c] = order[at:at + c]
+        at += c
+    if S > 4:
+        table[3, :1] = table[4, :1]  # a shared page
+    n_slots = max(int(np.maximum(more, 0).sum()) + extra, 0)
+    free = ref.free_pages(table, lens, P, n_pages)
+    t, n = i32(table), i32(lens)
+    fl, pool = torch.full((n_pages,), 99, dtype=torch.int32, device="cuda"), i32([5, 5])
+    uc.uc_page_free(t, n, P, fl, pool)
+    assert fl.tolist() == free + [-1] * (n_pages - len(free)) and pool.tolist() == [0, len(free)]
+    want = ref.step(lens, more, table, P, n_pages, free, [0, len(free)], n_slots)
+    outs = [torch.empty(k, dtype=torch.int32, device="cuda") for k in (S, S + 1, n_slots, 2)]
+    refused = torch.empty(S, dtype=torch.uint8, device="cuda")
+    for _ in range(2):  # with outputs of their own the call can be repeated
+        uc.uc_page_step(n, i32(more), t, P, fl, pool, *outs, refused)
+        assert np.array_equal(t.cpu().numpy(), want[0])
+        for got, w in zip([*outs, refused], [want[1], want[2], want[3], want[4], want[5]]):
+            assert got.tolist() == [int(x) for x in w]
+    if spare == 9:
+        assert any(want[5])
+    # in place
+    t2 = i32(table)
+    uc.uc_page_step(n, i32(more), t2, P, fl, pool, n, outs[1], outs[2], pool, refused)
+    assert n.tolist() == want[1] and pool.tolist() == want[4] and np.array_equal(t2.cpu().numpy(), want[0])
+
+
+# ---------------------------------------------------------------- attention
+
+ATTEND = [
+    # Hq, Hkv, D, group, P, dtype, lens, tokens
+    (1, 1, 128, 128, 16, "bf16", [1], [1]),
+    (28, 4, 128, 64, 16, "bf16", [1, 2, 15, 16, 17, 63, 64, 65, 777], [1] * 9),
+    (28, 4, 128, 32, 64, "bf16", [300, 0, 129, 4000, 64], [1, 0, 1, 1, 2]),
+    (8, 2, 64, 32, 32, "f16", [5, 1000, 33, 256, 31], [2, 4, 1, 3, 1]),
+    (8, 8, 64, 64, 128, "bf16", [500, 1, 1300], [16, 1, 9]),
+    (16, 1, 128, 128, 256, "f16", [2049, 70], [1, 1]),
+    (3, 3, 128, 32, 1024, "bf16", [3000], [5]),
+    # prompts: whole, chunked, one among single tokens, longer than the cache's rows (rows that see nothing)
+    (4, 1, 64, 64, 16, "bf16", [130], [130]),
+    (28, 4, 128, 64, 64, "bf16", [200, 333, 64], [200, 37, 3]),
+    (14, 2, 128, 32, 16, "f16", [90, 700, 1, 65], [1, 150, 1, 64]),
+    (8, 2, 64, 32, 32, "bf16", [10, 40, 0], [30, 40, 17]),
+    (12, 4, 128, 128, 128, "bf16", [260, 600], [256, 131]),
+]
+
+
+def run_attend(cache, table, lens, tokens, Hq, dtype, seed, q=None, ws=None, path=None, T_more=3):
+    """(o, lse, reference o, reference lse); T_more rows behind the last sequence."""
+    r = np.random.default_rng(seed)
+    start = np.concatenate([[0], np.cumsum(tokens)])
+    T = int(start[-1]) + T_more
+    D = cache.D
+    if q is None:  # a slice of a fused projection
+        q = torch.tensor(r.standard_normal((T, Hq + 2, D)) * 1.5, device="cuda").to(DT[dtype])[:, 1:Hq + 1]
+    o = torch.full((T, Hq, D), 5.0, device="cuda").to(DT[dtype])
+    lse = torch.full((T, Hq), 5.0, device="cuda")
+    scale = float(np.float32(D ** -0.5))
+    dev = cache.device(uc)
+    prev = uc.uc_set_path(path) if path is not None else None
+    try:
+        uc.uc_page_attend(dev, q, i32(start), i32(lens), i32(table), max(max(tokens), 1), scale, o, lse, ws=ws)
+        torch.cuda.synchronize()
+    finally:
+        if prev is not None:
+            uc.uc_set_path(prev)
+    want = ref.attend(cache, f64(q), start, lens, table, scale)
+    n = int(start[-1])
+    assert torch.all(o[n:] == 5.0) and torch.all(lse[n:] == 5.0)  # rows of no sequence stay
+    return o[:n], lse[:n], want[0][:n], want[1][:n]
+
+
+def check(o, lse, o_ref, lse_ref, dtype):
+    o, lse = f64(o), f64(lse)
+    empty = np.isneginf(lse_ref)
+    assert np.array_equal(empty, np.isneginf(lse)) and np.all(o[empty] == 0)
+    h = half(dtype)
+    err = np.abs(o - o_ref)
+    rel = np.linalg.norm(o - o_ref) / max(np.linalg.norm(o_ref), 1e-30)
+    print(f"max {err.max():.2e} rel {rel:.2e} lse {np.abs(lse[~empty] - lse_ref[~empty]).max(initial=0):.2e}", flush=True)
+    assert np.all(err <= 2e-3 + h * np.abs(o_ref))
+    assert rel <= 1e-3 + h
+    assert np.allclose(lse[~empty], lse_ref[~empty], rtol=1e-5, atol=1e-4)
+
+
+@pytest.mark.parametrize("path", ["auto", "valu"])
+@pytest.mark.parametrize("case", ATTEND, ids=[f"a{i}" for i in range(len(ATTEND))])
+def test_attention(case, path):
+    Hq, Hkv, D, group, P, dtype, lens, tokens = case
+    _case(test="attend", path=path, Hq=Hq, Hkv=Hkv, D=D, group=group, P=P, dtype=dtype, lens=lens, tokens=tokens)
+    cache, table = make_cache(lens, P, Hkv, D, group, sum(lens) + Hq)
+    got = run_attend(cache, table, lens, tokens, Hq, dtype, 7, path=uc.UC_PATH_VALU if path == "valu" else None)
+    name = uc.uc_last_kernel()
+    assert name == ("page_valu" if path == "valu" else
+                    "page_tokens" if max(tokens) * (Hq // Hkv) <= 16 else "page_valu"), name
+    check(*got, dtype)
+
+
+@pytest.mark.parametrize("Hkv,G,D", [(2, 4, 128), (1, 3, 64)])
+def test_attention_of_f32_queries(Hkv, G, D):
+    lens, tokens = [700, 1, 40, 0], [1, 1, 33, 2]
+    cache, table = make_cache(lens, 16, Hkv, D, 32, 11)
+    o, lse, o_ref, lse_ref = run_attend(cache, table, lens, tokens, Hkv * G, "f32", 3)
+    assert uc.uc_last_kernel() == "page_valu"
+    # binary32 throughout: sums of 700 terms, logits of 128
+    assert np.allclose(f64(o), o_ref, atol=2e-5)
+    fine = np.isfinite(lse_ref)
+    assert np.allclose(f64(lse)[fine], lse_ref[fine], rtol=2e-6, atol=2e-6)
+    assert np.all(np.isneginf(f64(lse)[~fine]))
+
+
+@pytest.mark.parametrize("tokens", [1, 40])
+def test_long_contexts_split_over_workgroups(tokens):
+    lens = [20000, 3, 9000]
+    cache, table = make_cache(lens, 64, 2, 128, 64, 21)
+    check(*run_attend(cache, table, lens, [tokens, 1, 1], 8, "bf16", 4), "bf16")
+
+
+@pytest.mark.parametrize("tokens", [1, 30])
+def test_many_sequences(tokens):
+    r = np.random.default_rng(2)
+    lens = [int(x) for x in r.integers(0, 90, 700)]
+    toks = [int(x) for x in r.integers(0, 2, 700)]
+    toks[350], lens[350] = tokens, 200
+    cache, table = make_cache(lens, 16, 1, 64, 32, 22)
+    check(*run_attend(cache, table, lens, toks, 4, "bf16", 5), "bf16")
+
+
+@pytest.mark.parametrize("tokens", [1, 20])
+def test_sharp_logits(tokens):
+    """Logits far apart: one key takes all, references rise step by step."""
+    lens = [1500]
+    cache, table = make_cache(lens, 32, 1, 128, 32, 23, scale=6.0)
+    o, lse, o_ref, lse_ref = run_attend(cache, table, lens, [tokens], 4, "bf16", 6)
+    # logits reach 500: a rounding of binary32 sums of 128 products there is 1e-4, and the values reach 30
+    assert np.all(np.abs(f64(o) - o_ref) <= half("bf16") * np.abs(o_ref) + 2e-2)
+    assert np.allclose(f64(lse), lse_ref, rtol=1e-5, atol=1e-4)
+
+
+@pytest.mark.parametrize("path", ["auto", "valu"])
+@pytest.mark.parametrize("tokens", [1, 24])
+def test_pages_outside_the_cache(tokens, path):
+    """An entry outside the cache spoils its own sequence only."""
+    lens = [100, 200, 100]
+    cache, table = make_cache(lens, 16, 2, 128, 64, 31)
+    good = np.array(table)
+    table[1, 2] = cache.n_pages + 5
+    table[0, 7:] = 1 << 30  # behind the sequence: not looked at
+    prev = uc.uc_set_path(uc.UC_PATH_VALU if path == "valu" else uc.UC_PATH_AUTO)
+    try:
+        start = np.concatenate([[0], np.cumsum([tokens] * 3)])
+        q = torch.randn(3 * tokens, 4, 128, device="cuda", dtype=torch.bfloat16)
+        o, lse = torch.empty_like(q), torch.empty(3 * tokens, 4, device="cuda")
+        uc.uc_page_attend(cache.device(uc), q, i32(start), i32(lens), i32(table), tokens, 0.088, o, lse)
+        torch.cuda.synchronize()
+    finally:
+        uc.uc_set_path(prev)
+    want, want_lse = ref.attend(cache, f64(q), start, lens, good, float(np.float32(0.088)))
+    assert torch.isnan(o[tokens:2 * tokens]).all() and torch.isnan(lse[tokens:2 * tokens]).all()
+    for a in (0, 2 * tokens):
+        check(o[a:a + tokens], lse[a:a + tokens], want[a:a + tokens], want_lse[a:a + tokens], "bf16")
+
+
+def test_starts_and_lengths_out_of_range():
+    """What the device holds is held to the arrays, not trusted."""
+    cache, table = make_cache([64, 64], 16, 1, 64, 32, 41)
+    q = torch.randn(6, 2, 64, device="cuda", dtype=torch.bfloat16)
+    o = torch.zeros_like(q)
+    for start, lens in (([-5, 3, 900], [64, 64]), ([0, 5, 2], [10 ** 9, -4]), ([6, 6, 6], [64, 64])):
+        uc.uc_page_attend(cache.device(uc), q, i32(start), i32(lens), i32(table), 6, 0.1, o)
+    torch.cuda.synchronize()
+
+
+def test_attention_replayed_from_a_graph_with_lengths_on_the_device():
+    Hq, Hkv, D, P, S = 8, 2, 128, 16, 5
+    lens = [3, 40, 200, 16, 90]
+    cache, table = make_cache(lens, P, Hkv, D, 64, 51, spare=40)
+    table = np.pad(table, ((0, 0), (0, 4)), constant_values=-1)
+    dev, t, n = cache.device(uc), i32(table), i32(lens)
+    free, pool = torch.empty(cache.n_pages, dtype=torch.int32, device="cuda"), i32([0, 0])
+    uc.uc_page_free(t, n, P, free, pool)
+    one, start, slots = i32([1] * S), i32([0] * (S + 1)), i32([0] * S)
+    refused = torch.zeros(S, dtype=torch.uint8, device="cuda")
+    k, v = (torch.randn(S, Hkv, D, device="cuda", dtype=torch.bfloat16) for _ in range(2))
+    q = torch.randn(S, Hq, D, device="cuda", dtype=torch.bfloat16)
+    o, lse = torch.empty_like(q), torch.empty(S, Hq, device="cuda")
+    ws = torch.empty(uc.uc_page_attend_workspace_size(dev, Hq, S, S, 1), dtype=torch.uint8, device="cuda")
+    before = [x.clone() for x in (t, n, pool, *dev.t.values())]
+
+    def step():
+        uc.uc_page_step(n, one, t, P, free, pool, n, start, slots, pool, refused)
+        uc.uc_page_append(dev, k, v, slots)
+        uc.uc_page_attend(dev, q, start, n, t, 1, 0.1, o, lse, ws=ws)
+
+    step()  # once eagerly, then back
+    torch.cuda.synchronize()
+    for x, y in zip((t, n, pool, *dev.t.values()), before):
+        x.copy_(y)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=side):
+        step()
+    torch.cuda.synchronize()
+    table_h, lens_h, pool_h = table, lens, pool.tolist()
+    free_h = free.tolist()
+    for i in range(20):
+        k.copy_(torch.randn(k.shape)), v.copy_(torch.randn(k.shape)), q.copy_(torch.randn(q.shape))
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        table_h, lens_h, start_h, slots_h, pool_h, ref_h = ref.step(lens_h, [1] * S, table_h, P, cache.n_pages, free_h,
+                                                                    pool_h, S)
+        assert not any(ref_h) and n.tolist() == lens_h and slots.tolist() == slots_h and pool.tolist() == pool_h
+        cache.append(k.float().cpu().numpy(), v.float().cpu().numpy(), slots_h)
+        want = ref.attend(cache, f64(q), start_h, lens_h, table_h, float(np.float32(0.1)))
+        check(o, lse, *want, "bf16")
+        torch.ones(1000, device="cuda").sum().item()  # work of the program's own between replays
+
+
+# ---------------------------------------------------------------- beams
+
+BEAMS = [  # R, W, V, dtype
+    (1, 1, 1, "f32"), (1, 4, 32003, "f32"), (3, 8, 5000, "bf16"), (7, 3, 997, "f16"), (2, 32, 40, "f32"),
+    (40, 5, 131, "bf16"), (1, 2, 200001, "bf16"), (2, 16, 65537, "f16"),
+]
+
+
+def select(x, score, done, eos, pad, inplace=False):
+    R, W, V = x.shape
+    out = score.clone() if inplace else torch.empty(R, W, device="cuda")
+    par, tok = (torch.empty(R, W, dtype=torch.int32, device="cuda") for _ in range(2))
+    dn = done.clone() if inplace else torch.empty(R, W, dtype=torch.uint8, device="cuda")
+    uc.uc_beam_select(x, out if inplace else score, dn if inplace else done, eos, pad, out, par, tok, dn)
+    torch.cuda.synchronize()
+    return [t.cpu().numpy() for t in (out, par, tok, dn)]
+
+
+def check_beams(got, want):
+    assert np.array_equal(got[1], want[1]) and np.array_equal(got[2], want[2])
+    assert np.array_equal(got[3] != 0, want[3])
+    # binary32 sums of exponentials (2^-24 a term, thousands of them), one rounding of the total
+    both = np.isneginf(want[0])
+    assert np.array_equal(both, np.isneginf(got[0]))
+    assert np.allclose(got[0][~both], want[0][~both], rtol=2 ** -23, atol=4e-6)
+
+
+@pytest.mark.parametrize("R,W,V,dtype", BEAMS)
+def test_beam_selection(R, W, V, dtype):
+    _case(test="beam", R=R, W=W, V=V, dtype=dtype)
+    r = np.random.default_rng(V)
+    x = torch.tensor(r.standard_normal((R, W, V + 3)) * 3, device="cuda").to(DT[dtype])[:, :, 2:V + 2]  # odd alignment
+    score = torch.tensor(r.standard_normal((R, W)) * 2 - 30, device="cuda").float()
+    done = torch.tensor(r.random((R, W)) < 0.2, device="cuda").to(torch.uint8)
+    eos, pad = min(2, V - 1), V // 2
+    want = ref.beam_select(f64(x), f64(score), done.cpu().numpy(), eos, pad)
+    for inplace in (False, True):
+        check_beams(select(x, score, done, eos, pad, inplace), want)
+
+
+def test_beam_selection_of_special_rows():
+    R, W, V = 8, 4, 3000
+    r = np.random.default_rng(9)
+    x = r.standard_normal((R, W, V)).astype(np.float32)
+    score = (r.standard_normal((R, W)) - 20).astype(np.float32)
+    done = np.zeros((R, W), np.uint8)
+    score[0, 1:] = -np.inf  # the first step: one live beam
+    x[1, 0, 5:] = -np.inf  # five tokens allowed, in every beam of the request but one
+    x[1, 1:, 7:] = -np.inf
+    x[2] = 1.0  # all alike: the lowest tokens
+    score[2] = -7.0
+    x[3, 2] = -np.inf  # a beam with nothing
+    x[4, 1, 17] = np.inf  # no finite normaliser
+    x[5, :, ::2] = np.nan
+    done[6] = 1
+    done[7, 1:] = 1
+    x[7, 0, 3:] = np.finfo(np.float32).min
+    want = ref.beam_select(x.astype(np.float64), score.astype(np.float64), done, 2, 0)
+    check_beams(select(torch.from_numpy(x).cuda(), torch.from_numpy(score).cuda(), torch.from_numpy(done).cuda(), 2, 0), want)
+    # nothing above -inf at all
+    x[:] = -np.inf
+    want = ref.beam_select(x.astype(np.float64), score.astype(np.float64), done, -1, 1)
+    check_beams(select(torch.from_numpy(x).cuda(), torch.from_numpy(score).cuda(), torch.from_numpy(done).cuda(), -1, 1), want)
+    # the type's lowest value everywhere: as good as any other constant
+    x[:] = np.finfo(np.float32).min
+    want = ref.beam_select(x.astype(np.float64), score.astype(np.float64), done, -1, 1)
+    check_beams(select(torch.from_numpy(x).cuda(), torch.from_numpy(score).cuda(), torch.from_numpy(done).cuda(), -1, 1), want)
+
+
+@pytest.mark.parametrize("order", ["rising", "falling"])
+def test_beam_selection_of_sorted_rows(order):
+    x = np.linspace(-4, 4, 6000, dtype=np.float32)[None, None].repeat(3, 1)
+    x = np.ascontiguousarray(x if order == "rising" else x[..., ::-1])
+    score = np.array([[-1.0, -1.0001, -3.0]], np.float32)
+    want = ref.beam_select(x.astype(np.float64), score.astype(np.float64), np.zeros((1, 3)), -1, 0)
+    got = select(torch.from_numpy(x).cuda(), torch.from_numpy(score).cuda(),
+                 torch.zeros(1, 3, dtype=torch.uint8, device="cuda"), -1, 0)
+    check_beams(got, want)
+
+
+@pytest.mark.parametrize("inplace", [False, True])
+@pytest.mark.parametrize("R,W,P,n,nb", [(1, 1, 16, 5, 3), (3, 4, 16, 33, 5), (2, 8, 64, 128, 2), (2, 32, 16, 700, 50),
+                                        (5, 5, 32, 0, 4), (1, 6, 16, 6000, 400)])
+def test_beam_reorder(R, W, P, n, nb, inplace):
+    _case(test="reorder", R=R, W=W, P=P, n=n, nb=nb)
+    r = np.random.default_rng(W + n)
+    table = r.permutation(R * W * nb).reshape(R * W, nb)
+    parent = r.integers(0, W, (R, W))
+    token = r.integers(0, 1000, (R, W))
+    hist = r.integers(0, 1000, (R * W, n + 4))
+    lens = [n] * (R * W)
+    t, h = i32(table), i32(hist)
+    t_out, h_out = (t, h) if inplace else (t.clone(), h.clone())
+    copies = torch.full((R * W, 3), 9, dtype=torch.int32, device="cuda")
+    uc.uc_beam_reorder(i32(parent), i32(token), t, i32(lens), P, t_out, copies, h, h_out, n)
+    want, want_copies = ref.beam_reorder(parent, table, lens, P)
+    assert np.array_equal(t_out.cpu().numpy(), want) and np.array_equal(copies.cpu().numpy(), want_copies)
+    rows = (np.arange(R)[:, None] * W + parent).ravel()
+    want_h = hist.copy()
+    want_h[:, :n] = hist[rows][:, :n]
+    want_h[:, n] = token.ravel()
+    assert np.array_equal(h_out.cpu().numpy(), want_h)
+    held = want[:, :-(-n // P)]
+    if n % P:  # the pages being filled stay private
+        assert len(set(held[:, -1].tolist())) == R * W
+
+
+# ---------------------------------------------------------------- together
+
+def test_beam_search_over_the_cache():
+    """Prompts, then a beam search: tables, appends, attention, selection and
+    reordering as a program runs them.  Every beam's cache must at every step
+    hold the rows of its own history, whose keys and values are a function of
+    (position, token) here, and attend over them."""
+    R, W, P, Hq, Hkv, D, group, V, steps = 2, 4, 16, 4, 2, 64, 32, 50, 40
+    S = R * W
+    r = np.random.default_rng(77)
+    rows_k, rows_v = (torch.tensor(r.standard_normal((200, V, Hkv, D)), device="cuda").bfloat16() for _ in range(2))
+    prompt = [37, 16]  # one ends inside a page, one at its end
+    nb, n_pages = 12, S * 12
+    cache = uc.page_cache(n_pages, P, Hkv, D, group)
+    for x in cache.t.values():
+        x.fill_(-1 if x.dtype == torch.int32 else 255)
+    table = torch.full((S, nb), -1, dtype=torch.int32, device="cuda")
+    n = torch.zeros(S, dtype=torch.int32, device="cuda")
+    free, pool = torch.empty(n_pages, dtype=torch.int32, device="cuda"), i32([0, 0])
+    refused = torch.zeros(S, dtype=torch.uint8, device="cuda")
+    hist = torch.zeros(S, 128, dtype=torch.int32, device="cuda")
+    ids = [torch.tensor(r.integers(0, V, m), device="cuda") for m in prompt]
+
+    # the prompts, into each request's first beam
+    more = i32([m if b == 0 else 0 for m in prompt for b in range(W)])
+    start, slots = i32([0] * (S + 1)), torch.empty(sum(prompt), dtype=torch.int32, device="cuda")
+    uc.uc_page_free(table, n, P, free, pool)
+    uc.uc_page_step(n, more, table, P, free, pool, n, start, slots, pool, refused)
+    k = torch.cat([rows_k[torch.arange(m, device="cuda"), x] for m, x in zip(prompt, ids)])
+    v = torch.cat([rows_v[torch.arange(m, device="cuda"), x] for m, x in zip(prompt, ids)])
+    uc.uc_page_append(cache, k, v, slots)
+    # the other beams share its full pages, and get a page of their own for the rest
+    for i, m in enumerate(prompt):
+        for b in range(1, W):
+            table[i * W + b, :m // P] = table[i * W, :m // P]
+            n[i * W + b] = m // P * P
+        hist[i * W:(i + 1) * W, :m] = ids[i].int()
+    more = i32([m % P if b else 0 for m in prompt for b in range(W)])
+    slots = torch.empty(int(more.sum()), dtype=torch.int32, device="cuda")
+    uc.uc_page_free(table, n, P, free, pool)
+    uc.uc_page_step(n, more, table, P, free, pool, n, start, slots, pool, refused)
+    assert not refused.any()
+
+    score = torch.full((R, W), -float("inf"), device="cuda")
+    score[:, 0] = 0.0
+    done = torch.zeros(R, W, dtype=torch.uint8, device="cuda")
+    par, tok = (torch.empty(R, W, dtype=torch.int32, device="cuda") for _ in range(2))
+    copies = torch.empty(S, 3, dtype=torch.int32, device="cuda")
+    one = i32([1] * S)
+    slots = torch.empty(S, dtype=torch.int32, device="cuda")
+    moved = 0
+    for i in range(steps):
+        # the two requests' histories have different lengths: reorder each by its own call
+        logits = torch.tensor(r.standard_normal((R, W, V)) * 2, device="cuda").float()
+        before, sc, dn = hist.clone(), f64(score), done.cpu().numpy()
+        uc.uc_beam_select(logits, score, done, -1, 0, score, par, tok, done)
+        want = ref.beam_select(f64(logits), sc, dn, -1, 0)
+        assert np.array_equal(par.cpu().numpy(), want[1]) and np.array_equal(tok.cpu().numpy(), want[2])
+        for j, m in enumerate(prompt):
+            a = slice(j * W, (j + 1) * W)
+            uc.uc_beam_reorder(par[j:j + 1], tok[j:j + 1], table[a], n[a], P, table[a], copies[a], hist[a], hist[a], m + i)
+        for s in range(S):
+            m = prompt[s // W] + i
+            assert hist[s, :m].tolist() == before[s // W * W + want[1].flat[s], :m].tolist()
+            assert hist[s, m] == want[2].flat[s]
+        moved += int((copies[:, 0] >= 0).sum())
+        uc.uc_page_free(table, n, P, free, pool)  # pages of beams that ended go back
+        uc.uc_page_step(n, one, table, P, free, pool, n, start, slots, pool, refused)
+        assert not refused.any()
+        pos = n.long() - 1
+        t = tok.flatten().long()
+        uc.uc_page_append(cache, rows_k[pos, t], rows_v[pos, t], slots, copies)
+        q = torch.tensor(r.standard_normal((S, Hq, D)), device="cuda").bfloat16()
+        o, lse = torch.empty_like(q), torch.empty(S, Hq, device="cuda")
+        uc.uc_page_attend(cache, q, start, n, table, 1, 0.125, o, lse)
+        # each beam against its own history
+        L = n.tolist()
+        for s in range(S):
+            own = ref.Cache(-(-L[s] // P), P, Hkv, D, group)
+            h = hist[s, :L[s]].long()
+            j = torch.arange(L[s], device="cuda")
+            own.append(rows_k[j, h].float().cpu().numpy(), rows_v[j, h].float().cpu().numpy(), range(L[s]))
+            w = ref.attend(own, f64(q[s:s + 1]), [0, 1], [L[s]], [np.arange(-(-L[s] // P))], 0.125)
+            check(o[s:s + 1], lse[s:s + 1], *w, "bf16")
+    assert moved > 10
+    # a request that ends gives its pages back
+    n[:W] = 0
+    uc.uc_page_free(table, n, P, free, pool)
+    assert pool.tolist()[1] == len(ref.free_pages(table.cpu().numpy(), n.tolist(), P, n_pages))
