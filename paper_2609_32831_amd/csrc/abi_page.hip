@@ -20,7 +20,7 @@ hipError_t launch_page_append(const PageCache& pc, const void* k, const void* v,
                               const int32_t* slots, const int32_t* copies, int n_copies, hipStream_t st);
 hipError_t launch_page_read(const PageCache& pc, const int32_t* slots, int T, void* kout, void* vout, int dt,
                             int64_t ld, hipStream_t st);
-size_t page_attend_workspace(const PageCache& pc, int G, int T, int S, int max_q);
+size_t page_attend_workspace(const PageCache& pc, int G, int S, int max_q);
 hipError_t launch_page_attend(const PageAttendArgs& a, int q_dt, int max_q, bool valu, void* ws, hipStream_t st);
 size_t beam_select_workspace(int R, int W, int V);
 hipError_t launch_beam_select(const void* logits, int dt, int64_t ld, const float* score, const uint8_t* done, int R,
@@ -145,7 +145,7 @@ uc_status uc_page_read(const uc_page_cache* cache, const int32_t* slots, int T, 
 size_t uc_page_attend_workspace_size(const uc_page_cache* cache, int Hq, int T, int S, int max_q) {
   PageCache pc;
   if (check_cache(cache, pc) || Hq < 1 || Hq % pc.Hkv || T < 0 || S < 1 || max_q < 1) return 0;
-  return page_attend_workspace(pc, Hq / pc.Hkv, T, S, max_q);
+  return page_attend_workspace(pc, Hq / pc.Hkv, S, max_q);
 }
 
 uc_status uc_page_attend(const uc_page_cache* cache, int Hq, const void* q, uc_dtype q_dt, int64_t q_ld, int T, int S,
@@ -167,7 +167,7 @@ uc_status uc_page_attend(const uc_page_cache* cache, int Hq, const void* q, uc_d
       (st = check_rows("o", o, q_dt, (int64_t)Hq * pc.D, (int64_t)Hq * pc.D)))
     return st;
   if (lse && !aligned4(lse)) return fail(UC_E_INVALID, "lse is not 4-byte aligned");
-  const size_t need = page_attend_workspace(pc, Hq / pc.Hkv, T, S, max_q);
+  const size_t need = page_attend_workspace(pc, Hq / pc.Hkv, S, max_q);
   if (!ws || !aligned16(ws) || ws_bytes < need)
     return fail(UC_E_WORKSPACE, "workspace %zu < %zu bytes, or not 16-byte aligned", ws_bytes, need);
   const PageAttendArgs a{pc, q_start, len, table, q, o, lse, q_ld, S, T, table_ld, Hq / pc.Hkv, sm_scale * kLog2e};

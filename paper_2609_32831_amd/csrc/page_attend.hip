@@ -166,10 +166,13 @@ struct Cut {
 };
 
 // Records: piece w leaves at most two, [2 w] of a sequence it continues and
-// [2 w + 1] of one it begins; ROWS x (D + 2) floats: l, m, o.
-template <int D, int ROWS>
-__device__ inline float* record(float* rec, int w, int Hkv, int h, bool begins) {
-  return rec + (((int64_t)w * Hkv + h) * 2 + begins) * ROWS * (D + 2);
+// [2 w + 1] of one it begins; ROWS rows of o (D floats, not yet divided by l),
+// m and l.
+template <int D>
+constexpr int kRec = D + 4;
+template <int D, int ROWS, class T>
+__device__ inline T* record(T* rec, int w, int Hkv, int h, bool begins) {
+  return rec + (((int64_t)w * Hkv + h) * 2 + begins) * ROWS * kRec<D>;
 }
 
 // ---------------------------------------------------------------- single tokens
@@ -514,10 +517,10 @@ __global__ __launch_bounds__(256, 2) void page_tokens_kernel(PageAttendArgs a, i
         put<QT>(a.o, at * D + d, ls == 0.0f ? 0.0f : y / ls);
         if (d == 0 && a.lse) a.lse[at] = lse_of(M, ls);
       } else {
-        out[r * (D + 2) + 2 + d] = y;
+        out[r * kRec<D> + d] = y;
         if (d == 0) {
-          out[r * (D + 2)] = M;
-          out[r * (D + 2) + 1] = ls;
+          out[r * kRec<D> + D] = M;
+          out[r * kRec<D> + D + 1] = ls;
         }
       }
     }
@@ -526,6 +529,381 @@ __global__ __launch_bounds__(256, 2) void page_tokens_kernel(PageAttendArgs a, i
     __syncthreads();  // LDS is written again
     before += units;
     u = before;
+  }
+}
+
+// ---------------------------------------------------------------- prompts
+// Blocks of 128 query rows of a KV head, each over the tiles that its last
+// row sees; the line is made of all blocks' tiles.  A workgroup's four waves
+// take 32 rows each and share the tile in LDS, where it stands as c * s in
+// bf16 (exact; the 4-bit rows are read and unpacked once per 128 rows); the
+// minima go through matrix instructions of their own,
+//   q . k += sum_g m_g sum(q_g),  o += sum_j p_j m_jg,
+// with sum(q_g) in three bf16 parts (24 bits).  Bound by the matrix and vector
+// units together: per 64 keys x 32 rows a wave issues 32 (QP 1) + 64 matrix
+// instructions of 16 cycles for the two products and 12 for the minima, and
+// about 500 vector instructions of 4 cycles (softmax, unpacking).
+constexpr int QROWS = 128;
+
+// blocks of a sequence in the prompt kernel
+__device__ inline int prompt_blocks(const Seq& x, int G) {
+  const int64_t rows = (int64_t)x.n * G;
+  return rows <= 16 ? 0 : (int)((rows + QROWS - 1) / QROWS);
+}
+// tiles of its block b, at least one
+__device__ inline int prompt_tiles(const Seq& x, int G, int b) {
+  const int64_t last = min((int64_t)x.n - 1, ((int64_t)b * QROWS + QROWS - 1) / G);
+  const int64_t sees = max((int64_t)0, min((int64_t)x.len, (int64_t)x.len - x.n + last + 1));
+  return (int)max((int64_t)1, (sees + KT - 1) / KT);
+}
+
+// before[s]: units of the sequences ahead of s, before[S]: all of them
+__global__ __launch_bounds__(1024) void page_plan_kernel(PageAttendArgs a, int64_t* __restrict__ before) {
+  __shared__ int64_t part[16];
+  const int lane = threadIdx.x & 63;
+  int64_t base = 0;
+  for (int s0 = 0; s0 < a.S; s0 += 1024) {
+    const int s = s0 + threadIdx.x;
+    Seq x{0, 0, 0};
+    if (s < a.S) x = seq_of(a, s);
+    const int blocks = prompt_blocks(x, a.G);
+    int64_t mine = 0;
+    // the wave counts one sequence after the other, a block per lane
+    for (uint64_t todo = __builtin_amdgcn_ballot_w64(blocks > 0); todo; todo &= todo - 1) {
+      const int from = __ffsll((unsigned long long)todo) - 1;
+      const Seq y{0, __shfl(x.n, from, 64), __shfl(x.len, from, 64)};
+      const int nb = __shfl(blocks, from, 64);
+      int64_t sum = 0;
+      for (int b = lane; b < nb; b += 64) sum += prompt_tiles(y, a.G, b);
+#pragma unroll
+      for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
+      if (lane == from) mine = sum;
+    }
+    int64_t total;
+    const int64_t upto = block_scan(mine, part, total);
+    if (s < a.S) before[s] = base + upto - mine;
+    base += total;
+  }
+  if (threadIdx.x == 0) before[a.S] = base;
+}
+
+template <int D>
+constexpr int kRow = 2 * D + 32;  // bytes of a staged row: 8 consecutive rows start in different 8-bank groups
+
+template <int D>
+struct PromptLds {
+  uint8_t k[KT * kRow<D>];
+  uint8_t v[KT * kRow<D>];
+  uint16_t km[KT][8];      // minima of a key, zeros behind them
+  uint16_t vm[4][KT + 8];  // minima of a value group, by key
+};
+
+// a word's eight codes times s as bf16
+__device__ inline u4 times(uint32_t w, float s) {
+  const uint32_t m = opaque(0x0F0F0F0Fu);
+  const uint32_t lo = w & m, hi = (w >> 4) & m;
+  float x[8];
+#pragma unroll
+  for (int b = 0; b < 4; ++b) {
+    x[2 * b] = (float)((lo >> (8 * b)) & 0xFFu) * s;
+    x[2 * b + 1] = (float)((hi >> (8 * b)) & 0xFFu) * s;
+  }
+  return u4{bf2(x[0], x[1]), bf2(x[2], x[3]), bf2(x[4], x[5]), bf2(x[6], x[7])};
+}
+
+template <int D, int NG, int QP>
+__global__ __launch_bounds__(256, 2) void page_prompt_kernel(PageAttendArgs a, int W_all,
+                                                             const int64_t* __restrict__ units,
+                                                             float* __restrict__ rec, Cut* __restrict__ cuts) {
+  constexpr int KS = D / 32, DT = D / 16;
+  __shared__ __attribute__((aligned(16))) PromptLds<D> L;
+  __shared__ int64_t s_part[16];
+  __shared__ int s_block;
+  __shared__ int64_t s_before;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int i16 = lane & 15, g4 = lane >> 4;
+  const int Hkv = a.pc.Hkv, h = blockIdx.x % Hkv, w = blockIdx.x / Hkv;
+  const int G = a.G, Hq = G * Hkv, lgP = a.pc.lgP;
+  if (threadIdx.x == 0) cuts[blockIdx.x] = Cut{-1, 0, 0, 0};
+  const int64_t U = units[a.S];
+  const int W = (int)min((int64_t)W_all, U);
+  if (w >= W) return;
+  const int64_t u0 = piece_first(U, w, W), u1 = piece_first(U, w + 1, W);
+  // the sequence and the block that hold unit u0
+  int s = 0;
+  for (int hi = a.S; hi - s > 1;) {
+    const int mid = (s + hi) >> 1;
+    if (units[mid] <= u0) s = mid;
+    else hi = mid;
+  }
+  Seq x = seq_of(a, s);
+  int nb = prompt_blocks(x, G);
+  {
+    int64_t base = units[s];
+    for (int b0 = 0; b0 < nb; b0 += 256) {
+      const int b = b0 + threadIdx.x;
+      const int64_t mine = b < nb ? prompt_tiles(x, G, b) : 0;
+      int64_t total;
+      const int64_t upto = base + block_scan(mine, s_part, total);
+      if (upto - mine <= u0 && u0 < upto) {
+        s_block = b;
+        s_before = upto - mine;
+      }
+      base += total;
+    }
+  }
+  // the slots behind a key's minima stay zero
+  for (int i = threadIdx.x; i < KT * 8; i += 256) (&L.km[0][0])[i] = 0;
+  __syncthreads();
+  int b = s_block;
+  int64_t before = s_before;
+
+  for (int64_t u = u0; u < u1;) {
+    const int tiles = prompt_tiles(x, G, b);
+    const int t0 = (int)(u - before), t1 = (int)min((int64_t)tiles, u1 - before);
+    const int rows = (int)min((int64_t)QROWS, (int64_t)x.n * G - (int64_t)b * QROWS);
+    const int32_t* trow = a.table + (int64_t)s * a.ld;
+
+    u4 qb[2][QP][KS], sqb[2];
+    int lim[2];
+    int64_t tok[2];  // the lane's query rows, among the rows of o
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      const int r = wave * 32 + c * 16 + i16;
+      const int rr = b * QROWS + min(r, rows - 1), i = rr / G, g = rr % G;
+      lim[c] = (int)max((int64_t)0, min((int64_t)x.len, (int64_t)x.len - x.n + i + 1));
+      tok[c] = (int64_t)(x.q0 + i) * Hq + h * G + g;
+      const int64_t base = (int64_t)(x.q0 + i) * a.q_ld + (int64_t)(h * G + g) * D + g4 * 8;
+      float sq[NG];
+#pragma unroll
+      for (int g = 0; g < NG; ++g) sq[g] = 0.0f;
+#pragma unroll
+      for (int t = 0; t < KS; ++t) {
+        const u4 raw = *reinterpret_cast<const u4*>(static_cast<const uint16_t*>(a.q) + base + t * 32);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float f0 = QP == 1 ? __uint_as_float(raw[e] << 16) : f16_to_f32((uint16_t)raw[e]);
+          const float f1 = QP == 1 ? __uint_as_float(raw[e] & 0xFFFF0000u) : f16_to_f32((uint16_t)(raw[e] >> 16));
+          sq[t * NG / KS] += f0 + f1;
+          if constexpr (QP == 1) {
+            qb[c][0][t][e] = raw[e];
+          } else {
+            const uint32_t hi = bf2(f0, f1);
+            qb[c][0][t][e] = hi;
+            qb[c][1][t][e] = bf2(f0 - __uint_as_float(hi << 16), f1 - __uint_as_float(hi & 0xFFFF0000u));
+          }
+        }
+      }
+      // sums in three bf16 parts: part g4 in this lane's slots
+      uint32_t bits[4] = {0, 0, 0, 0};
+#pragma unroll
+      for (int g = 0; g < NG; ++g) {
+        float y = sq[g];
+        y += __shfl_xor(y, 16, 64);
+        y += __shfl_xor(y, 32, 64);
+#pragma unroll
+        for (int p = 0; p < 2; ++p)
+          if (p < g4) y -= bf16_to_f32(f32_to_bf16_bits(y));
+        const uint32_t v = g4 < 3 ? f32_to_bf16_bits(y) : 0;
+        bits[g >> 1] |= v << (16 * (g & 1));
+      }
+      sqb[c] = u4{bits[0], bits[1], bits[2], bits[3]};
+    }
+    const int lim_all = (int)max((int64_t)0, (int64_t)x.len - x.n + (int64_t)b * QROWS / G + 1);
+
+    float m[2] = {kNone, kNone}, l[2] = {0.0f, 0.0f};
+    f4 acc[2][DT], low[2];
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      low[c] = f4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int d = 0; d < DT; ++d) acc[c][d] = f4{0.f, 0.f, 0.f, 0.f};
+    }
+    bool bad = false;
+
+    if (x.len > 0) {
+      // a thread's share of a tile: 16 bytes of codes of a row, of keys and of
+      // values (D = 128), of one of them (D = 64)
+      constexpr int CH = D / 32;
+      const int key = D == 128 ? threadIdx.x >> 2 : (threadIdx.x & 127) >> 1, ch = threadIdx.x % CH;
+      const bool do_k = D == 128 || threadIdx.x < 128, do_v = D == 128 || threadIdx.x >= 128;
+      u4 ck, cv;
+      uint32_t wk[NG], wv[NG];
+      auto page_for = [&](int t) { return page_of(trow, min(t * KT + key, x.len - 1), lgP, a.pc.n_pages); };
+      auto issue = [&](int t, int page) {
+        if (page < 0) bad = true;
+        const int64_t row = page_row(max(page, 0), Hkv, h, lgP, min(t * KT + key, x.len - 1));
+        if (do_k) {
+          ck = *reinterpret_cast<const u4*>(a.pc.codes_k + row * (D / 2) + ch * 16);
+          load_words<NG>(a.pc.scale_k + row * NG, wk);
+        }
+        if (do_v) {
+          cv = *reinterpret_cast<const u4*>(a.pc.codes_v + row * (D / 2) + ch * 16);
+          load_words<NG>(a.pc.scale_v + row * NG, wv);
+        }
+      };
+      issue(t0, page_for(t0));
+      for (int t = t0; t < t1; ++t) {
+        // stage the tile; rows past the sequence repeat its last one
+        if (do_k) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int wd = ch * 4 + i, step = wd % KS, g = wd / KS;  // channels 32 step + 8 g ..
+            float st = word_step(wk[0]);
+#pragma unroll
+            for (int n = 1; n < NG; ++n)
+              if (step * NG / KS == n) st = word_step(wk[n]);
+            *reinterpret_cast<u4*>(L.k + key * kRow<D> + (step * 4 + g) * 16) = times(ck[i], st);
+          }
+          if (ch == 0) {
+#pragma unroll
+            for (int n = 0; n < NG; ++n) L.km[key][n] = (uint16_t)(wk[n] >> 16);
+          }
+        }
+        if (do_v) {
+          float st = word_step(wv[0]);
+#pragma unroll
+          for (int n = 1; n < NG; ++n)
+            if (ch * NG / CH == n) st = word_step(wv[n]);
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            *reinterpret_cast<u4*>(L.v + key * kRow<D> + (ch * 4 + i) * 16) = times(cv[i], st);
+          if (ch == 0) {
+#pragma unroll
+            for (int n = 0; n < NG; ++n) L.vm[n][key] = (uint16_t)(wv[n] >> 16);
+          }
+        }
+        __syncthreads();
+        if (t + 1 < t1) issue(t + 1, page_for(t + 1));
+
+        // logits of keys 16 k + 4 g4 + j
+        f4 sc[2][4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const u4 km = *reinterpret_cast<const u4*>(&L.km[k * 16 + i16][0]);
+          sc[0][k] = mfma(km, sqb[0], f4{0.f, 0.f, 0.f, 0.f});
+          sc[1][k] = mfma(km, sqb[1], f4{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+          for (int st = 0; st < KS; ++st) {
+            const u4 ka = *reinterpret_cast<const u4*>(L.k + (k * 16 + i16) * kRow<D> + (st * 4 + g4) * 16);
+#pragma unroll
+            for (int p = 0; p < QP; ++p) {
+              sc[0][k] = mfma(ka, qb[0][p][st], sc[0][k]);
+              sc[1][k] = mfma(ka, qb[1][p][st], sc[1][k]);
+            }
+          }
+        }
+        const int r0 = t * KT;
+        const bool mask = r0 + KT > lim_all;
+        u4 hi[2][2], lo[2][2];
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          if (mask) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+#pragma unroll
+              for (int j = 0; j < 4; ++j)
+                if (r0 + k * 16 + g4 * 4 + j >= lim[c]) sc[c][k][j] = -INFINITY;
+          }
+          float mx = -INFINITY;
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) mx = fmaxf(mx, sc[c][k][j]);
+          mx *= a.scale_log2;
+          if (__builtin_amdgcn_ballot_w64(mx > m[c] + kLazy)) {
+            mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+            mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+            const float m_new = fmaxf(m[c], mx), alpha = __builtin_amdgcn_exp2f(m[c] - m_new);
+            m[c] = m_new;
+            l[c] *= alpha;
+            low[c] *= alpha;
+#pragma unroll
+            for (int d = 0; d < DT; ++d) acc[c][d] *= alpha;
+          }
+#pragma unroll
+          for (int half = 0; half < 2; ++half) {
+            float e[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              e[i] = __builtin_amdgcn_exp2f(fmaf(sc[c][2 * half + (i >> 2)][i & 3], a.scale_log2, -m[c]));
+              l[c] += e[i];
+            }
+            split_p(e, hi[c][half], lo[c][half]);
+          }
+        }
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          const uint16_t* vm = &L.vm[i16 & (NG - 1)][half * 32 + g4 * 4];
+          const uint2 v0 = *reinterpret_cast<const uint2*>(vm), v1 = *reinterpret_cast<const uint2*>(vm + 16);
+          const u4 va{v0.x, v0.y, v1.x, v1.y};
+#pragma unroll
+          for (int c = 0; c < 2; ++c) {
+            low[c] = mfma(va, hi[c][half], low[c]);
+            low[c] = mfma(va, lo[c][half], low[c]);
+          }
+          const char* vb = (const char*)L.v + (half * 32 + g4 * 4 + (i16 >> 2)) * kRow<D> + (i16 & 3) * 8;
+#pragma unroll
+          for (int d = 0; d < DT; ++d) {
+            const u4 vt = ds_tr(vb + d * 32, vb + 16 * kRow<D> + d * 32);
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+              acc[c][d] = mfma(vt, hi[c][half], acc[c][d]);
+              acc[c][d] = mfma(vt, lo[c][half], acc[c][d]);
+            }
+          }
+        }
+        __syncthreads();  // the tile's LDS is written again
+      }
+    }
+
+    const int any_bad = __syncthreads_or(bad);
+    const bool begins = before >= u0, ends = before + tiles <= u1;
+    float* out = record<D, QROWS>(rec, w, Hkv, h, begins);
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      float ls = l[c];
+      ls += __shfl_xor(ls, 16, 64);
+      ls += __shfl_xor(ls, 32, 64);
+      if (any_bad) ls = __builtin_nanf("");
+      const int r = wave * 32 + c * 16 + i16;
+      if (r >= rows) continue;
+      if (begins && ends) {
+        const float inv = ls == 0.0f ? 0.0f : 1.0f / ls;
+#pragma unroll
+        for (int d = 0; d < DT; ++d) {
+          f4 y = acc[c][d];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) y[j] = (y[j] + low[c][d * NG / DT]) * inv;
+          const uint2 z = QP == 1 ? uint2{bf2(y[0], y[1]), bf2(y[2], y[3])} : uint2{h2(y[0], y[1]), h2(y[2], y[3])};
+          *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.o) + tok[c] * D + d * 16 + g4 * 4) = z;
+        }
+        if (g4 == 0 && a.lse) a.lse[tok[c]] = lse_of(m[c], ls);
+      } else {
+#pragma unroll
+        for (int d = 0; d < DT; ++d) {
+          f4 y = acc[c][d];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) y[j] += low[c][d * NG / DT];
+          *reinterpret_cast<f4*>(out + r * kRec<D> + d * 16 + g4 * 4) = y;
+        }
+        if (g4 == 0) {
+          out[r * kRec<D> + D] = m[c];
+          out[r * kRec<D> + D + 1] = ls;
+        }
+      }
+    }
+    if (begins && !ends && threadIdx.x == 0)
+      cuts[blockIdx.x] = Cut{s, w, piece_of(U, before + tiles - 1, W), b * QROWS};
+    before += tiles;
+    u = before;
+    if (u < u1 && ++b == nb) {  // on to the next sequence that has blocks
+      b = 0;
+      do {
+        x = seq_of(a, ++s);
+        nb = prompt_blocks(x, G);
+      } while (nb == 0);
+    }
   }
 }
 
@@ -543,10 +921,10 @@ __global__ __launch_bounds__(256) void page_merge_kernel(PageAttendArgs a, const
     const int r = e / D, d = e % D;
     float M = kNone, l = 0.0f, y = 0.0f;
     for (int w = k.first; w <= k.last; ++w) {
-      const float* p = rec + (((int64_t)w * Hkv + h) * 2 + (w == k.first)) * ROWS * (D + 2) + r * (D + 2);
-      const float m_new = fmaxf(M, p[0]), old = exp2f(M - m_new), add = exp2f(p[0] - m_new);
-      l = l * old + p[1] * add;
-      y = y * old + p[2 + d] * add;
+      const float* p = record<D, ROWS>(rec, w, Hkv, h, w == k.first) + r * kRec<D>;
+      const float m_new = fmaxf(M, p[D]), old = exp2f(M - m_new), add = exp2f(p[D] - m_new);
+      l = l * old + p[D + 1] * add;
+      y = y * old + p[d] * add;
       M = m_new;
     }
     const int i = (k.block + r) / G, g = (k.block + r) % G;
@@ -559,40 +937,37 @@ __global__ __launch_bounds__(256) void page_merge_kernel(PageAttendArgs a, const
 }  // namespace
 
 // pieces of the line per KV head: two workgroups per CU in one round
-static int token_pieces(const PageCache& pc, int S, int ld) {
-  const int64_t most = (int64_t)S * std::max<int64_t>(1, (((int64_t)ld << pc.lgP) + KT - 1) / KT) / WAVES;
-  return (int)std::max<int64_t>(1, std::min<int64_t>(std::max(1, 2 * device_cus() / pc.Hkv), most));
+static int pieces(const PageCache& pc) { return std::max(1, 2 * device_cus() / pc.Hkv); }
+
+static size_t align_up(size_t x) { return (x + 255) & ~(size_t)255; }
+
+// cuts, the prompt kernel's sums of units, records (none where there is one
+// piece); the two kernels of a call use it one after the other
+static size_t records_at(const PageCache& pc, int S) {
+  return align_up((size_t)pieces(pc) * pc.Hkv * sizeof(Cut)) + align_up(((size_t)S + 1) * sizeof(int64_t));
 }
 
-size_t page_tokens_workspace(const PageCache& pc) {
-  const size_t W = std::max(1, 2 * device_cus() / pc.Hkv) * (size_t)pc.Hkv;
-  return ((W * sizeof(Cut) + 255) & ~(size_t)255) + W * 2 * 16 * (pc.D + 2) * sizeof(float);
+size_t page_attend_workspace(const PageCache& pc, int G, int S, int max_q) {
+  const size_t W = pieces(pc), rows = (int64_t)max_q * G > 16 ? QROWS : 16;
+  return records_at(pc, S) + (W > 1 ? W * pc.Hkv * 2 * rows * (pc.D + 4) * sizeof(float) : 0);
 }
 
-hipError_t launch_page_tokens(const PageAttendArgs& a, int q_dt, void* ws, hipStream_t st) {
-  const int W = token_pieces(a.pc, a.S, a.ld), n = W * a.pc.Hkv;
+template <int D, int NG, int QP>
+static void launch_matrix(const PageAttendArgs& a, int max_q, void* ws, hipStream_t st) {
+  constexpr int QT = QP == 1 ? UC_BF16 : UC_F16;
+  const int W = pieces(a.pc);
   Cut* cuts = (Cut*)ws;
-  float* rec = (float*)((char*)ws + (((size_t)n * sizeof(Cut) + 255) & ~(size_t)255));
-#define UC_TOKENS(DIM, NGR)                                                                                \
-  {                                                                                                        \
-    if (q_dt == UC_BF16) {                                                                                 \
-      hipLaunchKernelGGL((page_tokens_kernel<DIM, NGR, 1>), dim3(n), dim3(256), 0, st, a, W, rec, cuts);   \
-      hipLaunchKernelGGL((page_merge_kernel<DIM, 16, UC_BF16>), dim3(n, 2), dim3(256), 0, st, a, rec, cuts); \
-    } else {                                                                                               \
-      hipLaunchKernelGGL((page_tokens_kernel<DIM, NGR, 2>), dim3(n), dim3(256), 0, st, a, W, rec, cuts);   \
-      hipLaunchKernelGGL((page_merge_kernel<DIM, 16, UC_F16>), dim3(n, 2), dim3(256), 0, st, a, rec, cuts);  \
-    }                                                                                                      \
-  }
-  if (a.pc.D == 128) {
-    if (a.pc.ng == 4) UC_TOKENS(128, 4)
-    else if (a.pc.ng == 2) UC_TOKENS(128, 2)
-    else UC_TOKENS(128, 1)
-  } else {
-    if (a.pc.ng == 2) UC_TOKENS(64, 2)
-    else UC_TOKENS(64, 1)
-  }
-#undef UC_TOKENS
-  return hipGetLastError();
+  int64_t* units = (int64_t*)((char*)ws + align_up((size_t)W * a.pc.Hkv * sizeof(Cut)));
+  float* rec = (float*)((char*)ws + records_at(a.pc, a.S));
+  const int64_t most = a.S * std::max<int64_t>(1, (((int64_t)a.ld << a.pc.lgP) + KT - 1) / KT);  // tiles there can be
+  const int Wt = (int)std::max<int64_t>(1, std::min<int64_t>(W, most / WAVES)), n = Wt * a.pc.Hkv;
+  hipLaunchKernelGGL((page_tokens_kernel<D, NG, QP>), dim3(n), dim3(256), 0, st, a, Wt, rec, cuts);
+  if (Wt > 1) hipLaunchKernelGGL((page_merge_kernel<D, 16, QT>), dim3(n, 2), dim3(256), 0, st, a, rec, cuts);
+  if ((int64_t)max_q * a.G <= 16) return;
+  const int np = W * a.pc.Hkv;
+  hipLaunchKernelGGL(page_plan_kernel, dim3(1), dim3(1024), 0, st, a, units);
+  hipLaunchKernelGGL((page_prompt_kernel<D, NG, QP>), dim3(np), dim3(256), 0, st, a, W, units, rec, cuts);
+  if (W > 1) hipLaunchKernelGGL((page_merge_kernel<D, QROWS, QT>), dim3(np, 16), dim3(256), 0, st, a, rec, cuts);
 }
 
 hipError_t launch_page_valu(const PageAttendArgs& a, int q_dt, hipStream_t st) {
@@ -612,15 +987,24 @@ hipError_t launch_page_valu(const PageAttendArgs& a, int q_dt, hipStream_t st) {
   return hipGetLastError();
 }
 
-size_t page_attend_workspace(const PageCache& pc, int G, int T, int S, int max_q) { return page_tokens_workspace(pc); }
-
 hipError_t launch_page_attend(const PageAttendArgs& a, int q_dt, int max_q, bool valu, void* ws, hipStream_t st) {
-  if (valu || (int64_t)max_q * a.G > 16) {
+  if (valu) {
     set_last_kernel("page_valu");
     return launch_page_valu(a, q_dt, st);
   }
-  set_last_kernel("page_tokens");
-  return launch_page_tokens(a, q_dt, ws, st);
+  set_last_kernel((int64_t)max_q * a.G > 16 ? "page_prompt" : "page_tokens");
+#define UC_MATRIX(DIM, NGR) \
+  q_dt == UC_BF16 ? launch_matrix<DIM, NGR, 1>(a, max_q, ws, st) : launch_matrix<DIM, NGR, 2>(a, max_q, ws, st)
+  if (a.pc.D == 128) {
+    if (a.pc.ng == 4) UC_MATRIX(128, 4);
+    else if (a.pc.ng == 2) UC_MATRIX(128, 2);
+    else UC_MATRIX(128, 1);
+  } else {
+    if (a.pc.ng == 2) UC_MATRIX(64, 2);
+    else UC_MATRIX(64, 1);
+  }
+#undef UC_MATRIX
+  return hipGetLastError();
 }
 
 }  // namespace uc

@@ -54,4 +54,26 @@ __device__ inline int64_t page_row(int page, int Hkv, int h, int lgP, int r) {
   return ((((int64_t)page * Hkv + h) << lgP)) + (r & ((1 << lgP) - 1));
 }
 
+// inclusive scan over the workgroup (blockDim a multiple of 64, at most
+// 1024); total: the sum.  part: 16 values of LDS.
+template <class T>
+__device__ inline T block_scan(T x, T* part, T& total) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const T y = __shfl_up(x, o, 64);
+    if (lane >= o) x += y;
+  }
+  __syncthreads();  // part may still be read from an earlier scan
+  if (lane == 63) part[wave] = x;
+  __syncthreads();
+  T before = 0;
+  total = 0;
+  for (int w = 0; w < waves; ++w) {
+    if (w < wave) before += part[w];
+    total += part[w];
+  }
+  return x + before;
+}
+
 }  // namespace uc

@@ -10,32 +10,10 @@
 //
 // Both are bound by latency, not by bytes (a table of 1000 sequences of 64
 // pages is 256 KB).
-#include "uc_common.h"
+#include "page_common.h"
 
 namespace uc {
 namespace {
-
-// inclusive scan over the workgroup (blockDim a multiple of 64, at most
-// 1024); total: the sum.  part: 16 values of LDS.
-template <class T>
-__device__ inline T block_scan(T x, T* part, T& total) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const T y = __shfl_up(x, o, 64);
-    if (lane >= o) x += y;
-  }
-  __syncthreads();  // part may still be read from an earlier scan
-  if (lane == 63) part[wave] = x;
-  __syncthreads();
-  T before = 0;
-  total = 0;
-  for (int w = 0; w < waves; ++w) {
-    if (w < wave) before += part[w];
-    total += part[w];
-  }
-  return x + before;
-}
 
 __device__ inline int blocks_of(int n, int lgP) { return (int)(((int64_t)n + (1 << lgP) - 1) >> lgP); }
 

@@ -257,7 +257,7 @@ def test_attention(case, path):
     got = run_attend(cache, table, lens, tokens, Hq, dtype, 7, path=uc.UC_PATH_VALU if path == "valu" else None)
     name = uc.uc_last_kernel()
     assert name == ("page_valu" if path == "valu" else
-                    "page_tokens" if max(tokens) * (Hq // Hkv) <= 16 else "page_valu"), name
+                    "page_tokens" if max(tokens) * (Hq // Hkv) <= 16 else "page_prompt"), name
     check(*got, dtype)
 
 
