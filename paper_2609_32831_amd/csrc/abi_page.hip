@@ -160,6 +160,11 @@ uc_status uc_page_attend(const uc_page_cache* cache, int Hq, const void* q, uc_d
   if (!dtype_ok(q_dt)) return fail(UC_E_INVALID, "bad q dtype %d", q_dt);
   if (!(sm_scale > 0.0f) || !isfinite(sm_scale)) return fail(UC_E_INVALID, "sm_scale must be finite and > 0");
   if ((int64_t)T * Hq > INT32_MAX) return fail(UC_E_UNSUPPORTED, "too many query rows");
+  // units of work: tiles of 64 rows, once per 128 query rows
+  const int64_t tiles = ((int64_t)table_ld * cache->page_rows + 63) / 64 + 8;
+  if (tiles > INT32_MAX / 64 || tiles * ((int64_t)S + (int64_t)T * (Hq / pc.Hkv) / 128) > INT32_MAX)
+    return fail(UC_E_UNSUPPORTED, "tables of %d pages for %d sequences and %d tokens hold too much work for one call",
+                table_ld, S, T);
   if ((st = check_ints("q_start", q_start)) || (st = check_ints("len", len)) || (st = check_ints("table", table)))
     return st;
   if (T == 0) return ok();

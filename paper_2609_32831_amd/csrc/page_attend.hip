@@ -148,16 +148,25 @@ __global__ __launch_bounds__(256) void page_attend_valu_kernel(PageAttendArgs a)
 }
 
 // ---------------------------------------------------------------- the line of tiles
-// Pieces of the line: unit u of U belongs to piece (((u + 1) W - 1) / U).
-__device__ inline int64_t piece_first(int64_t U, int w, int W) { return U * w / W; }
-__device__ inline int piece_of(int64_t U, int64_t u, int W) { return (int)(((u + 1) * W - 1) / U); }
+// U units cut into W pieces that differ by one unit at most, the longer ones
+// first (a call has fewer than 2^31 units, checked on the host).
+struct Line {
+  int per, more, W;
+  __device__ Line(int U, int pieces) : per(U / pieces), more(U % pieces), W(pieces) {}
+  __device__ int first(int w) const { return w * per + min(w, more); }
+  __device__ int piece_of(int u) const {  // the piece that holds unit u
+    const int edge = more * (per + 1);
+    return u < edge ? u / (per + 1) : more + (u - edge) / per;
+  }
+};
 
 // units of a sequence in the single-token kernel: its tiles, at least one so
-// that a row that sees nothing is written too; none where the prompt kernel
-// takes it
+// that a row that sees nothing is written too, behind kStart units that stand
+// for what a sequence costs beside them; none where the prompt kernel takes it
+constexpr int kStart = 8;
+__device__ inline int tiles_of(int rows) { return rows <= KT ? 1 : (int)(((uint32_t)rows + KT - 1) / KT); }
 __device__ inline int token_units(const Seq& x, int G) {
-  if (x.n == 0 || (int64_t)x.n * G > 16) return 0;
-  return max(1, (int)(((int64_t)x.len + KT - 1) / KT));
+  return x.n == 0 || (int64_t)x.n * G > 16 ? 0 : kStart + tiles_of(x.len);
 }
 
 // a sequence cut into pieces first .. last; rows of the call it stands for
@@ -177,22 +186,14 @@ __device__ inline T* record(T* rec, int w, int Hkv, int h, bool begins) {
 
 // ---------------------------------------------------------------- single tokens
 // codes of a word -> four pairs of bf16 (128 + code): pair i holds codes i
-// and i + 4
-__device__ inline u4 pairs(uint32_t w) {
-  const uint32_t m = 0x000F000Fu, k = 0x43004300u;
-  return u4{(w & m) | k, ((w >> 4) & m) | k, ((w >> 8) & m) | k, ((w >> 12) & m) | k};
-}
-
-template <int D>
-struct TileCodes {
-  static constexpr int VL = D / 32;  // 16-byte loads of a wave's share of values
-  uint32_t k[4][D / 32];             // four key blocks x the words of a lane
-  u4 v[VL];
-};
-
-template <int NG>
-struct TileWords {
-  uint32_t k[NG], v[NG];
+// and i + 4.  The two constants come in registers, where one instruction ands
+// and ors.
+struct Magic {
+  uint32_t mask, base;
+  __device__ Magic() : mask(opaque(0x000F000Fu)), base(opaque(0x43004300u)) {}
+  __device__ u4 pairs(uint32_t w) const {
+    return u4{(w & mask) | base, ((w >> 4) & mask) | base, ((w >> 8) & mask) | base, ((w >> 12) & mask) | base};
+  }
 };
 
 template <int N>
@@ -208,6 +209,19 @@ __device__ inline void load_words(const uint32_t* p, uint32_t (&w)[N]) {
   }
 }
 
+// D/32 words of codes, read once per call: past the caches
+typedef uint32_t u2 __attribute__((ext_vector_type(2)));
+template <int N>
+__device__ inline void load_codes(const uint8_t* p, uint32_t (&w)[N]) {
+  if constexpr (N == 4) {
+    const u4 x = __builtin_nontemporal_load(reinterpret_cast<const u4*>(p));
+    w[0] = x[0], w[1] = x[1], w[2] = x[2], w[3] = x[3];
+  } else {
+    const u2 x = __builtin_nontemporal_load(reinterpret_cast<const u2*>(p));
+    w[0] = x[0], w[1] = x[1];
+  }
+}
+
 template <int D, int NG>
 struct WaveLds {
   static constexpr int VROW = D / 2 + 8;  // bytes of a staged row of values
@@ -216,83 +230,140 @@ struct WaveLds {
   uint8_t codes[KT * VROW];
 };
 
-// D, NG: head dim and groups of a row; QP: bf16 parts of a query element
+// D, NG: head dim and groups of a row; QP: bf16 parts of a query element.
+//
+// A wave's tile is four blocks of 16 keys, each within one page (pages are 16
+// rows or more), so a block's codes are one contiguous piece of the cache
+// behind a scalar address.  Block b's product rows are its keys, and lane
+// group g4 holds those of keys 16 b + 4 g4 + j; the transposing reads of the
+// values take their rows in that order.
 template <int D, int NG, int QP>
 __global__ __launch_bounds__(256, 2) void page_tokens_kernel(PageAttendArgs a, int W_all, float* __restrict__ rec,
                                                              Cut* __restrict__ cuts) {
-  constexpr int KS = D / 32;       // matrix steps over the channels
-  constexpr int DT = D / 16;       // tiles of 16 output channels
-  constexpr int GS = KS / NG > 0 ? KS / NG : 1;
+  constexpr int KS = D / 32;  // matrix steps over the channels, words of a lane's codes of a row
+  constexpr int DT = D / 16;  // tiles of 16 output channels
+  constexpr int GS = KS / NG;
   constexpr int QT = QP == 1 ? UC_BF16 : UC_F16;
   using Lds = WaveLds<D, NG>;
   constexpr size_t kTiles = sizeof(Lds) * WAVES, kMerge = sizeof(float) * WAVES * 16 * (D + 2);
   __shared__ __attribute__((aligned(16))) char lds[kTiles > kMerge ? kTiles : kMerge];
-  __shared__ int64_t s_units[256];
-  __shared__ int64_t s_part[WAVES];
-  __shared__ int s_bucket;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int i16 = lane & 15, g4 = lane >> 4;
   const int Hkv = a.pc.Hkv, h = blockIdx.x % Hkv, w = blockIdx.x / Hkv;
-  const int G = a.G, Hq = G * Hkv, lgP = a.pc.lgP;
+  const int G = a.G, Hq = G * Hkv, lgP = a.pc.lgP, P1 = (1 << lgP) - 1;
+  const Magic magic;
+  if (threadIdx.x == 0) cuts[blockIdx.x] = Cut{-1, 0, 0, 0};
 
-  // this piece of the line: thread i counts sequences i c .. i c + c - 1
-  const int c = (a.S + 255) / 256;
-  int64_t mine = 0;
-  for (int s = threadIdx.x * c; s < min(a.S, (int)(threadIdx.x + 1) * c); ++s) mine += token_units(seq_of(a, s), G);
-  int64_t upto = mine;
+  // this piece of the line; lane i counts sequences i c .. i c + c - 1
+  const int c = (a.S + 63) / 64;
+  Seq x{0, 0, 0};
+  int mine = 0;
+  for (int s = lane * c; s < min(a.S, (lane + 1) * c); ++s) {
+    x = seq_of(a, s);
+    mine += token_units(x, G);
+  }
+  int upto = mine;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
-    const int64_t y = __shfl_up(upto, o, 64);
+    const int y = __shfl_up(upto, o, 64);
     if (lane >= o) upto += y;
   }
-  if (lane == 63) s_part[wave] = upto;
-  __syncthreads();
-  int64_t U = 0;
-  for (int i = 0; i < WAVES; ++i) {
-    if (i < wave) upto += s_part[i];
-    U += s_part[i];
-  }
-  if (threadIdx.x == 0) cuts[blockIdx.x] = Cut{-1, 0, 0, 0};
+  const int U = __builtin_amdgcn_readlane(upto, 63);
   if (U == 0) return;
-  // a tile per wave at least
-  const int W = (int)max((int64_t)1, min((int64_t)W_all, U / WAVES));
-  if (w >= W) return;
-  const int64_t u0 = piece_first(U, w, W), u1 = piece_first(U, w + 1, W);
-  s_units[threadIdx.x] = upto - mine;
-  if (upto - mine <= u0 && u0 < upto) s_bucket = threadIdx.x;
-  __syncthreads();
-  int s = s_bucket * c;
-  int64_t before = s_units[s_bucket];  // units before sequence s
+  // a sequence and a tile per wave at least
+  const Line line(U, max(1, min(W_all, U / (kStart + WAVES))));
+  if (w >= line.W) return;
+  const int u0 = line.first(w), u1 = line.first(w + 1);
+  const int bucket = __builtin_ctzll(__builtin_amdgcn_ballot_w64(upto > u0));
+  int s = bucket * c, before = __builtin_amdgcn_readlane(upto - mine, bucket);  // units before sequence s
+  if (c == 1) {
+    x = Seq{__builtin_amdgcn_readlane(x.q0, bucket), __builtin_amdgcn_readlane(x.n, bucket),
+            __builtin_amdgcn_readlane(x.len, bucket)};
+  } else {
+    x = seq_of(a, s);
+  }
   Lds& L = *reinterpret_cast<Lds*>(lds + wave * sizeof(Lds));
 
-  for (int64_t u = u0; u < u1; ++s) {
-    const Seq x = seq_of(a, s);
-    const int units = token_units(x, G);
-    if (before + units <= u) {
+  // The sequence at hand: tiles [t0, t1) of it lie in this piece.
+  int units = 0, t0 = 0, t1 = 0, page = 0, page_next = 0, last16 = 0;
+  const int32_t* trow = nullptr;
+  u4 raw[KS];                                    // the lane's query row
+  uint32_t ck[4][KS], cv[4][KS], wk[NG], wv[NG];  // a tile
+  bool bad = false;
+  // page of the lane's block of a tile; tiles past the range repeat its last
+  auto page_for = [&](int t) {
+    return x.len > 0 ? page_of(trow, min(min(t, t1 - 1) * KT + g4 * 16, last16), lgP, a.pc.n_pages) : 0;
+  };
+  // cache row of block b of tile t
+  auto block_row = [&](int t, int pg, int b) {
+    const int pb = max(__builtin_amdgcn_readlane(pg, 16 * b), 0);
+    return (((int64_t)pb * Hkv + h) << lgP) + (min(t * KT + 16 * b, last16) & P1);
+  };
+  auto issue_keys = [&](int t, int pg) {
+#pragma unroll
+    for (int b = 0; b < 4; ++b)
+      load_codes<KS>(a.pc.codes_k + block_row(t, pg, b) * (D / 2) + (uint32_t)(i16 * (D / 2) + g4 * (D / 8)), ck[b]);
+  };
+  auto issue_values = [&](int t, int pg) {
+    if (t * KT + g4 * 16 < x.len && pg < 0) bad = true;
+#pragma unroll
+    for (int b = 0; b < 4; ++b)
+      load_codes<KS>(a.pc.codes_v + block_row(t, pg, b) * (D / 2) + (uint32_t)(lane * (D / 8)), cv[b]);
+    const int64_t row = (((int64_t)max(pg, 0) * Hkv + h) << lgP) + (min(t * KT + g4 * 16, last16) & P1) + i16;
+    load_words<NG>(a.pc.scale_k + row * NG, wk);
+    load_words<NG>(a.pc.scale_v + row * NG, wv);
+  };
+  // on to the first sequence from s on with tiles in [u, u1); false if there
+  // is none.  Its pages and queries are asked for.
+  auto open = [&](int u) {
+    for (;;) {
+      units = token_units(x, G);
+      if (before + units > u) break;
       before += units;
-      continue;
+      if (before >= u1 || s + 1 >= a.S) return false;
+      x = seq_of(a, ++s);
     }
-    const int t0 = (int)(u - before), t1 = (int)min((int64_t)units, u1 - before);  // tiles [t0, t1) of sequence s
-    const int nq = x.n * G;
-    const int32_t* trow = a.table + (int64_t)s * a.ld;
+    if (before + kStart >= u1) return false;
+    t0 = max(0, u - before - kStart);
+    t1 = min(units, u1 - before) - kStart;
+    trow = a.table + (int64_t)s * a.ld;
+    last16 = (x.len - 1) & ~15;  // first row of the last 16
+    page = page_for(t0 + wave);
+    page_next = page_for(t0 + wave + WAVES);
+    const int r = min(i16, x.n * G - 1);
+    const uint16_t* q = static_cast<const uint16_t*>(a.q) + (int64_t)(x.q0 + r / G) * a.q_ld +
+                        (int64_t)(h * G + r % G) * D + g4 * 8;
+#pragma unroll
+    for (int t = 0; t < KS; ++t) raw[t] = *reinterpret_cast<const u4*>(q + t * 32);
+    return true;
+  };
+  // its first tile's loads
+  auto first = [&]() {
+    bad = false;
+    if (x.len > 0 && t0 + wave < t1) {
+      issue_values(t0 + wave, page);
+      issue_keys(t0 + wave, page);
+    }
+  };
+  if (!open(u0)) return;
+  first();
 
+  for (;;) {
+    const int nq = x.n * G;
     // queries: the operand's channel order pairs codes i and i + 4
     u4 qb[QP][KS];
     float sq[NG];  // sum of the group's channels, all of them in every lane
 #pragma unroll
     for (int g = 0; g < NG; ++g) sq[g] = 0.0f;
     {
-      const int r = min(i16, nq - 1);
-      const int64_t base = (int64_t)(x.q0 + r / G) * a.q_ld + (int64_t)(h * G + r % G) * D + g4 * 8;
 #pragma unroll
       for (int t = 0; t < KS; ++t) {
-        u4 raw = *reinterpret_cast<const u4*>(static_cast<const uint16_t*>(a.q) + base + t * 32);
-        if (i16 >= nq) raw = u4{0, 0, 0, 0};
+        if (i16 >= nq) raw[t] = u4{0, 0, 0, 0};
         float f[8];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          f[2 * e] = QP == 1 ? __uint_as_float(raw[e] << 16) : f16_to_f32((uint16_t)raw[e]);
-          f[2 * e + 1] = QP == 1 ? __uint_as_float(raw[e] & 0xFFFF0000u) : f16_to_f32((uint16_t)(raw[e] >> 16));
+          f[2 * e] = QP == 1 ? __uint_as_float(raw[t][e] << 16) : f16_to_f32((uint16_t)raw[t][e]);
+          f[2 * e + 1] = QP == 1 ? __uint_as_float(raw[t][e] & 0xFFFF0000u) : f16_to_f32((uint16_t)(raw[t][e] >> 16));
           sq[t / GS] += f[2 * e] + f[2 * e + 1];
         }
 #pragma unroll
@@ -319,74 +390,42 @@ __global__ __launch_bounds__(256, 2) void page_tokens_kernel(PageAttendArgs a, i
     for (int g = 0; g < NG; ++g) low[g] = 0.0f;
 #pragma unroll
     for (int d = 0; d < DT; ++d) acc[d] = f4{0.f, 0.f, 0.f, 0.f};
-    bool bad = false;
 
     if (x.len > 0) {
-      // pages of the lane's group of 16 keys (keys 16 g4 .. of the tile)
-      auto page_for = [&](int t) {
-        const int r = min(t * KT + g4 * 16, (x.len - 1) & ~15);
-        return page_of(trow, r, lgP, a.pc.n_pages);
-      };
-      TileCodes<D> tc;
-      TileWords<NG> tw;
-      auto issue = [&](int t, int page) {
-        if (t * KT + g4 * 16 < x.len && page < 0) bad = true;
-        page = max(page, 0);
-        const int r = min(t * KT + g4 * 16, (x.len - 1) & ~15);  // first row of the lane's group
-        const int64_t first = page_row(page, Hkv, h, lgP, r);      // its index in the cache
-        // keys: block b holds keys 16 (i16 / 4) + 4 b + i16 % 4, so that the
-        // product's rows 4 g4 .. + 3 of the four blocks are keys 16 g4 .. + 15
-        const int64_t kf = __shfl(first, (i16 >> 2) * 16, 64) + (i16 & 3);
-        const uint32_t* kc = (const uint32_t*)a.pc.codes_k + kf * (D / 8) + g4 * KS;
+      int t = t0 + wave;
+      for (; t < t1; t += WAVES) {
+        const int tn = t + WAVES;
+        const bool more = tn < t1;
+        // stage the tile: values as codes, words as floats; rows behind the
+        // sequence hold anything, so their words become zeros
+        {
+          const bool in = t * KT + lane < x.len;
+          uint8_t* dst = L.codes + (lane >> 2) * Lds::VROW + (lane & 3) * (D / 8);
 #pragma unroll
-        for (int b = 0; b < 4; ++b) {
-          if constexpr (KS == 4) {
-            const u4 x4 = *reinterpret_cast<const u4*>(kc + b * 4 * (D / 8));
-            tc.k[b][0] = x4[0], tc.k[b][1] = x4[1], tc.k[b][2] = x4[2], tc.k[b][3] = x4[3];
-          } else {
-            const uint2 x2 = *reinterpret_cast<const uint2*>(kc + b * 4 * (D / 8));
-            tc.k[b][0] = x2.x, tc.k[b][1] = x2.y;
+          for (int b = 0; b < 4; ++b) {
+#pragma unroll
+            for (int e = 0; e < KS; e += 2)
+              *reinterpret_cast<uint2*>(dst + b * 16 * Lds::VROW + e * 4) = uint2{cv[b][e], cv[b][e + 1]};
+          }
+#pragma unroll
+          for (int g = 0; g < NG; ++g) {
+            const uint32_t xk = in ? wk[g] : 0, xv = in ? wv[g] : 0;
+            L.k[0][g][lane] = word_step(xk);
+            L.k[1][g][lane] = word_min(xk);
+            L.v[0][g][lane] = word_step(xv);
+            L.v[1][g][lane] = fmaf(-128.0f, word_step(xv), word_min(xv));
           }
         }
-        // values: load i covers 64 / VL keys, whole rows
-        constexpr int CH = D / 32;  // 16-byte chunks of a row
-#pragma unroll
-        for (int i = 0; i < TileCodes<D>::VL; ++i) {
-          const int key = i * (KT / TileCodes<D>::VL) + lane / CH;
-          const int64_t vf = __shfl(first, (key >> 4) * 16, 64) + (key & 15);
-          tc.v[i] = *reinterpret_cast<const u4*>(a.pc.codes_v + vf * (D / 2) + (lane % CH) * 16);
-        }
-        load_words<NG>(a.pc.scale_k + (first + i16) * NG, tw.k);
-        load_words<NG>(a.pc.scale_v + (first + i16) * NG, tw.v);
-        if (t * KT + lane >= x.len) {  // rows behind the sequence hold anything
-#pragma unroll
-          for (int g = 0; g < NG; ++g) tw.k[g] = tw.v[g] = 0;
-        }
-      };
-
-      int t = t0 + wave;
-      if (t < t1) issue(t, page_for(t));
-      for (; t < t1; t += WAVES) {
-        // stage the tile: values as codes, words as floats
-        constexpr int CH = D / 32;
-#pragma unroll
-        for (int i = 0; i < TileCodes<D>::VL; ++i) {
-          const int key = i * (KT / TileCodes<D>::VL) + lane / CH;
-          uint2* dst = reinterpret_cast<uint2*>(L.codes + key * Lds::VROW + (lane % CH) * 16);
-          dst[0] = uint2{tc.v[i][0], tc.v[i][1]};
-          dst[1] = uint2{tc.v[i][2], tc.v[i][3]};
-        }
-#pragma unroll
-        for (int g = 0; g < NG; ++g) {
-          L.k[0][g][lane] = word_step(tw.k[g]);
-          L.k[1][g][lane] = word_min(tw.k[g]);
-          const float sv = word_step(tw.v[g]);
-          L.v[0][g][lane] = sv;
-          L.v[1][g][lane] = fmaf(-128.0f, sv, word_min(tw.v[g]));
-        }
         __builtin_amdgcn_wave_barrier();
+        // the next tile's loads, as registers become free; its page was read a
+        // tile ago
+        const int page_now = page_next;
+        if (more) {
+          issue_values(tn, page_now);
+          page_next = page_for(tn + WAVES);
+        }
 
-        // logits: p[b][j] of key 16 g4 + 4 b + j
+        // logits: p[4 b + j] of key 16 b + 4 g4 + j
         float p[16];
 #pragma unroll
         for (int b = 0; b < 4; ++b) {
@@ -397,12 +436,12 @@ __global__ __launch_bounds__(256, 2) void page_tokens_kernel(PageAttendArgs a, i
             f4 dot = f4{z, z, z, z};
 #pragma unroll
             for (int t2 = g * GS; t2 < (g + 1) * GS; ++t2) {
-              const u4 kb = pairs(tc.k[b][t2]);
+              const u4 kb = magic.pairs(ck[b][t2]);
 #pragma unroll
               for (int qp = 0; qp < QP; ++qp) dot = mfma(kb, qb[qp][t2], dot);
             }
-            const f4 st = *reinterpret_cast<const f4*>(&L.k[0][g][g4 * 16 + b * 4]);
-            const f4 mn = *reinterpret_cast<const f4*>(&L.k[1][g][g4 * 16 + b * 4]);
+            const f4 st = *reinterpret_cast<const f4*>(&L.k[0][g][b * 16 + g4 * 4]);
+            const f4 mn = *reinterpret_cast<const f4*>(&L.k[1][g][b * 16 + g4 * 4]);
 #pragma unroll
             for (int j = 0; j < 4; ++j) sum[j] = fmaf(st[j], dot[j], fmaf(mn[j], sq[g], sum[j]));
           }
@@ -411,13 +450,12 @@ __global__ __launch_bounds__(256, 2) void page_tokens_kernel(PageAttendArgs a, i
         }
         const int r0 = t * KT;
         if (r0 + KT > lim_all) {
+          asm volatile("");  // a branch, not sixteen selects per tile
 #pragma unroll
           for (int e = 0; e < 16; ++e)
-            if (r0 + g4 * 16 + e >= lim) p[e] = -INFINITY;
+            if (r0 + (e >> 2) * 16 + g4 * 4 + (e & 3) >= lim) p[e] = -INFINITY;
         }
-        // the next tile's loads: the codes of this one's keys are used up
-        const int tn = t + WAVES;
-        if (tn < t1) issue(tn, page_for(tn));
+        if (more) issue_keys(tn, page_now);
 
         // softmax against a lazily raised reference maximum
         float mx = p[0];
@@ -443,11 +481,11 @@ __global__ __launch_bounds__(256, 2) void page_tokens_kernel(PageAttendArgs a, i
         // O^T += V^T P, group by group
 #pragma unroll
         for (int g = 0; g < NG; ++g) {
-          float e1[8], e2[8];  // (key i, key i + 4) pairs of keys 0 .. 7 and 8 .. 15
+          float e1[8], e2[8];  // pairs (j, j + 4) of a lane's keys 0 .. 7 and 8 .. 15
 #pragma unroll
           for (int b = 0; b < 4; ++b) {
-            const f4 st = *reinterpret_cast<const f4*>(&L.v[0][g][g4 * 16 + b * 4]);
-            const f4 mn = *reinterpret_cast<const f4*>(&L.v[1][g][g4 * 16 + b * 4]);
+            const f4 st = *reinterpret_cast<const f4*>(&L.v[0][g][b * 16 + g4 * 4]);
+            const f4 mn = *reinterpret_cast<const f4*>(&L.v[1][g][b * 16 + g4 * 4]);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
               const float ps = p[b * 4 + j] * st[j];
@@ -458,13 +496,13 @@ __global__ __launch_bounds__(256, 2) void page_tokens_kernel(PageAttendArgs a, i
           u4 h1, l1, h2, l2;
           split_p(e1, h1, l1);
           split_p(e2, h2, l2);
+          const uint8_t* row = L.codes + ((i16 >> 2) * 16 + g4 * 4 + (i16 & 3)) * Lds::VROW;
 #pragma unroll
           for (int d = g * (DT / NG); d < (g + 1) * (DT / NG); ++d) {
             typedef int v2i __attribute__((ext_vector_type(2)));
             typedef __attribute__((address_space(3))) v2i lds_v2i;
-            const v2i cw = __builtin_amdgcn_ds_read_tr4_b64_v2i32(
-                (lds_v2i*)(L.codes + (g4 * 16 + i16) * Lds::VROW + d * 8));
-            const u4 va = pairs((uint32_t)cw[0]), vb = pairs((uint32_t)cw[1]);
+            const v2i cw = __builtin_amdgcn_ds_read_tr4_b64_v2i32((lds_v2i*)(row + d * 8));
+            const u4 va = magic.pairs((uint32_t)cw[0]), vb = magic.pairs((uint32_t)cw[1]);
             acc[d] = mfma(va, h1, acc[d]);
             acc[d] = mfma(va, l1, acc[d]);
             acc[d] = mfma(vb, h2, acc[d]);
@@ -475,7 +513,16 @@ __global__ __launch_bounds__(256, 2) void page_tokens_kernel(PageAttendArgs a, i
       }
     }
 
-    // merge the waves
+    // the next sequence's loads are under way while this one's waves merge
+    const Seq now = x;
+    const int s_now = s, from = before + kStart, to = before + units;  // its tiles' units
+    bool more = to < u1 && s + 1 < a.S;
+    const bool any = bad;
+    if (more) {
+      before = to;
+      x = seq_of(a, ++s);
+      more = open(to);
+    }
     l += __shfl_xor(l, 16, 64);
     l += __shfl_xor(l, 32, 64);
 #pragma unroll
@@ -483,7 +530,7 @@ __global__ __launch_bounds__(256, 2) void page_tokens_kernel(PageAttendArgs a, i
       low[g] += __shfl_xor(low[g], 16, 64);
       low[g] += __shfl_xor(low[g], 32, 64);
     }
-    const int any_bad = __syncthreads_or(bad);
+    const int any_bad = __syncthreads_or(any);
     float* mo = reinterpret_cast<float*>(lds);  // [WAVES][16][D]
     float* ml = mo + WAVES * 16 * D;            // [WAVES][16] m, then l
     if (g4 == 0) {
@@ -497,23 +544,24 @@ __global__ __launch_bounds__(256, 2) void page_tokens_kernel(PageAttendArgs a, i
       for (int j = 0; j < 4; ++j) y[j] += low[d / (DT / NG)];
       *reinterpret_cast<f4*>(&mo[(wave * 16 + i16) * D + d * 16 + g4 * 4]) = y;
     }
+    if (more) first();
     __syncthreads();
-    const bool begins = before >= u0, ends = before + units <= u1;
+    const bool begins = from >= u0, ends = to <= u1;
     float* out = record<D, 16>(rec, w, Hkv, h, begins);
     for (int e = threadIdx.x; e < nq * D; e += blockDim.x) {
       const int r = e / D, d = e % D;
-      float M = kNone, wt[WAVES], ls = 0.0f, y = 0.0f;
+      float M = kNone, ls = 0.0f, y = 0.0f;
 #pragma unroll
       for (int i = 0; i < WAVES; ++i) M = fmaxf(M, ml[i * 16 + r]);
 #pragma unroll
       for (int i = 0; i < WAVES; ++i) {
-        wt[i] = exp2f(ml[i * 16 + r] - M);
-        ls = fmaf(wt[i], ml[WAVES * 16 + i * 16 + r], ls);
-        y = fmaf(wt[i], mo[(i * 16 + r) * D + d], y);
+        const float wt = exp2f(ml[i * 16 + r] - M);
+        ls = fmaf(wt, ml[WAVES * 16 + i * 16 + r], ls);
+        y = fmaf(wt, mo[(i * 16 + r) * D + d], y);
       }
       if (any_bad) ls = __builtin_nanf("");
       if (begins && ends) {
-        const int64_t at = (int64_t)(x.q0 + r / G) * Hq + h * G + r % G;
+        const int64_t at = (int64_t)(now.q0 + r / G) * Hq + h * G + r % G;
         put<QT>(a.o, at * D + d, ls == 0.0f ? 0.0f : y / ls);
         if (d == 0 && a.lse) a.lse[at] = lse_of(M, ls);
       } else {
@@ -524,11 +572,9 @@ __global__ __launch_bounds__(256, 2) void page_tokens_kernel(PageAttendArgs a, i
         }
       }
     }
-    if (begins && !ends && threadIdx.x == 0)
-      cuts[blockIdx.x] = Cut{s, w, piece_of(U, before + units - 1, W), 0};
+    if (begins && !ends && threadIdx.x == 0) cuts[blockIdx.x] = Cut{s_now, w, line.piece_of(to - 1), 0};
+    if (!more) break;
     __syncthreads();  // LDS is written again
-    before += units;
-    u = before;
   }
 }
 
@@ -554,33 +600,33 @@ __device__ inline int prompt_blocks(const Seq& x, int G) {
 __device__ inline int prompt_tiles(const Seq& x, int G, int b) {
   const int64_t last = min((int64_t)x.n - 1, ((int64_t)b * QROWS + QROWS - 1) / G);
   const int64_t sees = max((int64_t)0, min((int64_t)x.len, (int64_t)x.len - x.n + last + 1));
-  return (int)max((int64_t)1, (sees + KT - 1) / KT);
+  return tiles_of((int)sees);
 }
 
 // before[s]: units of the sequences ahead of s, before[S]: all of them
-__global__ __launch_bounds__(1024) void page_plan_kernel(PageAttendArgs a, int64_t* __restrict__ before) {
-  __shared__ int64_t part[16];
+__global__ __launch_bounds__(1024) void page_plan_kernel(PageAttendArgs a, int* __restrict__ before) {
+  __shared__ int part[16];
   const int lane = threadIdx.x & 63;
-  int64_t base = 0;
+  int base = 0;
   for (int s0 = 0; s0 < a.S; s0 += 1024) {
     const int s = s0 + threadIdx.x;
     Seq x{0, 0, 0};
     if (s < a.S) x = seq_of(a, s);
     const int blocks = prompt_blocks(x, a.G);
-    int64_t mine = 0;
+    int mine = 0;
     // the wave counts one sequence after the other, a block per lane
     for (uint64_t todo = __builtin_amdgcn_ballot_w64(blocks > 0); todo; todo &= todo - 1) {
       const int from = __ffsll((unsigned long long)todo) - 1;
       const Seq y{0, __shfl(x.n, from, 64), __shfl(x.len, from, 64)};
       const int nb = __shfl(blocks, from, 64);
-      int64_t sum = 0;
+      int sum = 0;
       for (int b = lane; b < nb; b += 64) sum += prompt_tiles(y, a.G, b);
 #pragma unroll
       for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
       if (lane == from) mine = sum;
     }
-    int64_t total;
-    const int64_t upto = block_scan(mine, part, total);
+    int total;
+    const int upto = block_scan(mine, part, total);
     if (s < a.S) before[s] = base + upto - mine;
     base += total;
   }
@@ -613,22 +659,21 @@ __device__ inline u4 times(uint32_t w, float s) {
 
 template <int D, int NG, int QP>
 __global__ __launch_bounds__(256, 2) void page_prompt_kernel(PageAttendArgs a, int W_all,
-                                                             const int64_t* __restrict__ units,
+                                                             const int* __restrict__ units,
                                                              float* __restrict__ rec, Cut* __restrict__ cuts) {
   constexpr int KS = D / 32, DT = D / 16;
   __shared__ __attribute__((aligned(16))) PromptLds<D> L;
-  __shared__ int64_t s_part[16];
-  __shared__ int s_block;
-  __shared__ int64_t s_before;
+  __shared__ int s_part[16], s_block, s_before;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int i16 = lane & 15, g4 = lane >> 4;
   const int Hkv = a.pc.Hkv, h = blockIdx.x % Hkv, w = blockIdx.x / Hkv;
   const int G = a.G, Hq = G * Hkv, lgP = a.pc.lgP;
   if (threadIdx.x == 0) cuts[blockIdx.x] = Cut{-1, 0, 0, 0};
-  const int64_t U = units[a.S];
-  const int W = (int)min((int64_t)W_all, U);
-  if (w >= W) return;
-  const int64_t u0 = piece_first(U, w, W), u1 = piece_first(U, w + 1, W);
+  const int U = units[a.S];
+  if (U == 0) return;
+  const Line line(U, min(W_all, U));
+  if (w >= line.W) return;
+  const int u0 = line.first(w), u1 = line.first(w + 1);
   // the sequence and the block that hold unit u0
   int s = 0;
   for (int hi = a.S; hi - s > 1;) {
@@ -638,13 +683,14 @@ __global__ __launch_bounds__(256, 2) void page_prompt_kernel(PageAttendArgs a, i
   }
   Seq x = seq_of(a, s);
   int nb = prompt_blocks(x, G);
+  if (threadIdx.x == 0) s_block = -1;
   {
-    int64_t base = units[s];
+    int base = units[s];
     for (int b0 = 0; b0 < nb; b0 += 256) {
       const int b = b0 + threadIdx.x;
-      const int64_t mine = b < nb ? prompt_tiles(x, G, b) : 0;
-      int64_t total;
-      const int64_t upto = base + block_scan(mine, s_part, total);
+      const int mine = b < nb ? prompt_tiles(x, G, b) : 0;
+      int total;
+      const int upto = base + block_scan(mine, s_part, total);
       if (upto - mine <= u0 && u0 < upto) {
         s_block = b;
         s_before = upto - mine;
@@ -656,11 +702,12 @@ __global__ __launch_bounds__(256, 2) void page_prompt_kernel(PageAttendArgs a, i
   for (int i = threadIdx.x; i < KT * 8; i += 256) (&L.km[0][0])[i] = 0;
   __syncthreads();
   int b = s_block;
-  int64_t before = s_before;
+  if (b < 0) return;  // starts that overlap so often that the sums passed their type
+  int before = s_before;
 
-  for (int64_t u = u0; u < u1;) {
+  for (int u = u0; u < u1;) {
     const int tiles = prompt_tiles(x, G, b);
-    const int t0 = (int)(u - before), t1 = (int)min((int64_t)tiles, u1 - before);
+    const int t0 = u - before, t1 = min(tiles, u1 - before);
     const int rows = (int)min((int64_t)QROWS, (int64_t)x.n * G - (int64_t)b * QROWS);
     const int32_t* trow = a.table + (int64_t)s * a.ld;
 
@@ -894,21 +941,24 @@ __global__ __launch_bounds__(256, 2) void page_prompt_kernel(PageAttendArgs a, i
       }
     }
     if (begins && !ends && threadIdx.x == 0)
-      cuts[blockIdx.x] = Cut{s, w, piece_of(U, before + tiles - 1, W), b * QROWS};
+      cuts[blockIdx.x] = Cut{s, w, line.piece_of(before + tiles - 1), b * QROWS};
     before += tiles;
     u = before;
     if (u < u1 && ++b == nb) {  // on to the next sequence that has blocks
       b = 0;
       do {
-        x = seq_of(a, ++s);
+        if (++s >= a.S) return;
+        x = seq_of(a, s);
         nb = prompt_blocks(x, G);
       } while (nb == 0);
     }
   }
 }
 
-// one workgroup per cut: its pieces' records in order, ROWS query rows from
-// row `block` of the sequence on
+// One workgroup per cut and group of its rows: its pieces' records in order,
+// ROWS query rows from row `block` of the sequence on.  A thread takes four
+// channels; a row's references and sums come first, so that the records' loads
+// do not wait for one another.
 template <int D, int ROWS, int QT>
 __global__ __launch_bounds__(256) void page_merge_kernel(PageAttendArgs a, const float* __restrict__ rec,
                                                          const Cut* __restrict__ cuts) {
@@ -917,19 +967,44 @@ __global__ __launch_bounds__(256) void page_merge_kernel(PageAttendArgs a, const
   const int Hkv = a.pc.Hkv, h = blockIdx.x % Hkv, G = a.G, Hq = G * Hkv;
   const Seq x = seq_of(a, k.seq);
   const int rows = (int)min((int64_t)ROWS, (int64_t)x.n * G - k.block);
-  for (int e = blockIdx.y * blockDim.x + threadIdx.x; e < rows * D; e += gridDim.y * blockDim.x) {
-    const int r = e / D, d = e % D;
-    float M = kNone, l = 0.0f, y = 0.0f;
-    for (int w = k.first; w <= k.last; ++w) {
-      const float* p = record<D, ROWS>(rec, w, Hkv, h, w == k.first) + r * kRec<D>;
-      const float m_new = fmaxf(M, p[D]), old = exp2f(M - m_new), add = exp2f(p[D] - m_new);
-      l = l * old + p[D + 1] * add;
-      y = y * old + p[d] * add;
+  constexpr int TR = D / 4;  // threads of a row
+  const int d = threadIdx.x % TR * 4;
+  for (int r = blockIdx.y * (256 / TR) + threadIdx.x / TR; r < rows; r += gridDim.y * (256 / TR)) {
+    float M = kNone, l = 0.0f;
+    f4 y = f4{0.f, 0.f, 0.f, 0.f};
+    constexpr int N = 8;  // records at a time
+    for (int w0 = k.first; w0 <= k.last; w0 += N) {
+      f4 v[N];
+      float m[N], ls[N];
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const int w = min(w0 + i, k.last);
+        const float* p = record<D, ROWS>(rec, w, Hkv, h, w == k.first) + r * kRec<D>;
+        v[i] = *reinterpret_cast<const f4*>(p + d);
+        m[i] = w0 + i <= k.last ? p[D] : kNone;
+        ls[i] = w0 + i <= k.last ? p[D + 1] : 0.0f;
+      }
+      float m_new = M;
+#pragma unroll
+      for (int i = 0; i < N; ++i) m_new = fmaxf(m_new, m[i]);
+      const float old = exp2f(M - m_new);
+      l *= old;
+      y *= old;
       M = m_new;
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const float wt = w0 + i <= k.last ? exp2f(m[i] - M) : 0.0f;
+        l = fmaf(ls[i], wt, l);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) y[j] = fmaf(v[i][j], wt, y[j]);
+      }
     }
     const int i = (k.block + r) / G, g = (k.block + r) % G;
     const int64_t at = (int64_t)(x.q0 + i) * Hq + h * G + g;
-    put<QT>(a.o, at * D + d, l == 0.0f ? 0.0f : y / l);
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+    y *= inv;
+    const uint2 z = QT == UC_BF16 ? uint2{bf2(y[0], y[1]), bf2(y[2], y[3])} : uint2{h2(y[0], y[1]), h2(y[2], y[3])};
+    *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.o) + at * D + d) = z;
     if (d == 0 && a.lse) a.lse[at] = lse_of(M, l);
   }
 }
@@ -944,7 +1019,7 @@ static size_t align_up(size_t x) { return (x + 255) & ~(size_t)255; }
 // cuts, the prompt kernel's sums of units, records (none where there is one
 // piece); the two kernels of a call use it one after the other
 static size_t records_at(const PageCache& pc, int S) {
-  return align_up((size_t)pieces(pc) * pc.Hkv * sizeof(Cut)) + align_up(((size_t)S + 1) * sizeof(int64_t));
+  return align_up((size_t)pieces(pc) * pc.Hkv * sizeof(Cut)) + align_up(((size_t)S + 1) * sizeof(int));
 }
 
 size_t page_attend_workspace(const PageCache& pc, int G, int S, int max_q) {
@@ -957,10 +1032,10 @@ static void launch_matrix(const PageAttendArgs& a, int max_q, void* ws, hipStrea
   constexpr int QT = QP == 1 ? UC_BF16 : UC_F16;
   const int W = pieces(a.pc);
   Cut* cuts = (Cut*)ws;
-  int64_t* units = (int64_t*)((char*)ws + align_up((size_t)W * a.pc.Hkv * sizeof(Cut)));
+  int* units = (int*)((char*)ws + align_up((size_t)W * a.pc.Hkv * sizeof(Cut)));
   float* rec = (float*)((char*)ws + records_at(a.pc, a.S));
   const int64_t most = a.S * std::max<int64_t>(1, (((int64_t)a.ld << a.pc.lgP) + KT - 1) / KT);  // tiles there can be
-  const int Wt = (int)std::max<int64_t>(1, std::min<int64_t>(W, most / WAVES)), n = Wt * a.pc.Hkv;
+  const int Wt = (int)std::max<int64_t>(1, std::min<int64_t>(W, (most + (int64_t)kStart * a.S) / (kStart + WAVES))), n = Wt * a.pc.Hkv;
   hipLaunchKernelGGL((page_tokens_kernel<D, NG, QP>), dim3(n), dim3(256), 0, st, a, Wt, rec, cuts);
   if (Wt > 1) hipLaunchKernelGGL((page_merge_kernel<D, 16, QT>), dim3(n, 2), dim3(256), 0, st, a, rec, cuts);
   if ((int64_t)max_q * a.G <= 16) return;
