@@ -14,8 +14,6 @@
 // it; another child takes over the last page of a beam without children, and
 // the list of copies says which rows are to be copied there (every layer's
 // append does so before attention).  So no page is taken or given up.
-#include <algorithm>
-
 #include "mfma_util.h"
 #include "uc_common.h"
 
@@ -24,55 +22,132 @@ namespace {
 
 constexpr int kMaxW = UC_MAX_BEAMS;
 
-struct Best {  // lane i holds the i-th best of the wave (value descending, index ascending)
-  float v;
-  int i;
-  float last_v;  // the W-th best, in every lane
-  int last_i;
+// Cross-lane steps without LDS.  `old` is what lanes without a source keep.
+template <int CTRL, int ROWS = 0xF>
+__device__ inline uint32_t dpp(uint32_t old, uint32_t x) {
+  return (uint32_t)__builtin_amdgcn_update_dpp((int)old, (int)x, CTRL, ROWS, 0xF, false);
+}
+__device__ inline float lane_of(float x, int i) {
+  return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), i));
+}
+__device__ inline int lane_of(int x, int i) { return __builtin_amdgcn_readlane(x, i); }
+// f over the wave in six steps, in lane 63 (then in every lane)
+template <class F>
+__device__ inline void wave_fold(F f) {
+  f.template step<0x111, 0xF>();
+  f.template step<0x112, 0xF>();
+  f.template step<0x114, 0xF>();
+  f.template step<0x118, 0xF>();
+  f.template step<0x142, 0xA>();
+  f.template step<0x143, 0xC>();
+}
+struct MaxStep {
+  float& x;
+  template <int CTRL, int ROWS>
+  __device__ void step() {
+    const uint32_t u = __float_as_uint(x);
+    x = fmaxf(x, __uint_as_float(dpp<CTRL, ROWS>(u, u)));
+  }
+};
+__device__ inline float max_of_wave(float x) {
+  wave_fold(MaxStep{x});
+  return lane_of(x, 63);
+}
+
+// An element as one number, the larger the earlier: value descending, then
+// index ascending.
+__device__ inline uint64_t key_of(float v, int i) {
+  const uint32_t u = __float_as_uint(v + 0.0f);  // -0 is 0
+  return (uint64_t)(u ^ ((uint32_t)((int)u >> 31) | 0x80000000u)) << 32 | (uint32_t)(INT32_MAX - i);
+}
+__device__ inline float value_of(uint64_t key) {
+  const uint32_t u = (uint32_t)(key >> 32);
+  return __uint_as_float(u ^ (u >> 31 ? 0x80000000u : 0xFFFFFFFFu));
+}
+__device__ inline int index_of(uint64_t key) { return INT32_MAX - (int)(uint32_t)key; }
+
+struct KeyStep {
+  uint64_t& k;
+  template <int CTRL, int ROWS>
+  __device__ void step() {
+    const uint32_t lo = (uint32_t)k, hi = (uint32_t)(k >> 32);
+    const uint64_t y = (uint64_t)dpp<CTRL, ROWS>(hi, hi) << 32 | dpp<CTRL, ROWS>(lo, lo);
+    k = y > k ? y : k;
+  }
 };
 
-__device__ inline bool before(float v, int i, float v2, int i2) { return v > v2 || (v == v2 && i < i2); }
+// What a wave has gathered (LDS), and what an element has to pass to join: W
+// elements of the split have a value of v or more, or key or more.
+constexpr int kCap = 576;  // W and eight elements of 64 lanes
+struct Floor {
+  float v;
+  uint64_t key;
+  int count;
+};
 
-__device__ inline void insert(Best& b, int W, int lane, float v, int i) {
-  const int at = __popcll(__builtin_amdgcn_ballot_w64(lane < W && before(b.v, b.i, v, i)));
-  const float uv = __shfl_up(b.v, 1, 64);
-  const int ui = __shfl_up(b.i, 1, 64);
-  if (lane > at) b.v = uv, b.i = ui;
-  if (lane == at) b.v = v, b.i = i;
-  b.last_v = __shfl(b.v, W - 1, 64);
-  b.last_i = __shfl(b.i, W - 1, 64);
+// keeps the W best of what the wave has gathered (W of them at least)
+__device__ inline void cut_down(uint64_t* g, Floor& f, int W, int lane) {
+  __builtin_amdgcn_wave_barrier();
+  uint64_t mine = 0;
+  for (int k = 0; k < W; ++k) {
+    uint64_t best = 0;
+    for (int j = lane; j < f.count; j += 64) best = g[j] > best ? g[j] : best;
+    uint64_t top = best;
+    wave_fold(KeyStep{top});
+    top = (uint64_t)(uint32_t)lane_of((int)(top >> 32), 63) << 32 | (uint32_t)lane_of((int)top, 63);
+    if (best == top)
+      for (int j = lane; j < f.count; j += 64)
+        if (g[j] == top) g[j] = 0;
+    if (lane == k) mine = top;
+    f.key = top;
+  }
+  __builtin_amdgcn_wave_barrier();
+  if (lane < W) g[lane] = mine;
+  f.v = value_of(f.key);
+  f.count = W;
+  __builtin_amdgcn_wave_barrier();
 }
 
-template <int DT>
-__device__ inline float elem(const void* p, int64_t i) {
-  return fmaxf(load_elem(p, DT, i), -INFINITY);  // a NaN counts as -inf
+// The sum's terms are 2^(c x - r), c = log2(e) as a float and r the rounded
+// product of c and the largest of the split's first logits: one multiply-add
+// and one exponential an element.  r is taken as it is, so its rounding
+// cancels; it must not grow past what an exponent holds, so it stands for at
+// most 2^30.  Where the sum leaves its type (a logit beyond that, or 88 above
+// the first ones, or a NaN) the split is summed again, by differences.
+constexpr float kHeld = 1073741824.0f;
+__device__ inline float held(float x) { return __builtin_amdgcn_fmed3f(x, -kHeld, kHeld); }  // NaN: -kHeld
+__device__ inline float ranked(float x) { return x != x ? -INFINITY : x; }
+
+// the n-th largest of the wave's values
+__device__ inline float nth_largest(float x, int n, int lane) {
+  for (;;) {
+    const float t = max_of_wave(x);
+    if (--n == 0) return t;
+    const uint64_t who = __builtin_amdgcn_ballot_w64(x == t);
+    if (lane == __ffsll((unsigned long long)who) - 1) x = -INFINITY;
+  }
 }
 
-// N elements per lane, e-th one at index base + e; those past n are -inf
+// N elements per lane, e-th one at index base + e (none of the lane's if !in)
 template <int N>
-__device__ inline void consume(const float (&x)[N], int base, int n, int W, int lane, Best& b, float& m, float& s) {
+__device__ inline void consume(const float (&x)[N], int base, bool in, int W, int lane, uint64_t* g, Floor& f, float r,
+                               float& s) {
   float mx = x[0];
 #pragma unroll
-  for (int e = 1; e < N; ++e) mx = fmaxf(mx, x[e]);
-  if (mx > m) {
-    s *= exp2f((m - mx) * kLog2e);
-    m = mx;
-  }
-  // differences first: the rounding of m * log2(e) would reach every term
-  const float ref = m == -INFINITY ? 0.0f : m;
+  for (int e = 1; e < N; ++e) mx = fmaxf(mx, x[e]);  // (a NaN loses)
+  float sum = 0.0f;
 #pragma unroll
-  for (int e = 0; e < N; ++e) s += __builtin_amdgcn_exp2f((x[e] - ref) * kLog2e);
-  if (__builtin_amdgcn_ballot_w64(n > 0 && mx >= b.last_v)) {
+  for (int e = 0; e < N; ++e) sum += __builtin_amdgcn_exp2f(fmaf(x[e], kLog2e, -r));
+  s += in ? sum : 0.0f;
+  if (__builtin_amdgcn_ballot_w64(in && !(mx < f.v))) {
+    if (f.count + 64 * N > kCap) cut_down(g, f, W, lane);
 #pragma unroll
     for (int e = 0; e < N; ++e) {
-      uint64_t todo = __builtin_amdgcn_ballot_w64(e < n && before(x[e], base + e, b.last_v, b.last_i));
-      while (todo) {
-        const int from = __ffsll((unsigned long long)todo) - 1;
-        todo &= todo - 1;
-        const float v = __shfl(x[e], from, 64);
-        const int i = __shfl(base, from, 64) + e;
-        if (before(v, i, b.last_v, b.last_i)) insert(b, W, lane, v, i);
-      }
+      if (!__builtin_amdgcn_ballot_w64(in && !(x[e] < f.v))) continue;
+      const uint64_t key = key_of(ranked(x[e]), base + e);
+      const uint64_t join = __builtin_amdgcn_ballot_w64(in && key > f.key);
+      if (join >> lane & 1) g[f.count + __popcll(join & ((1ull << lane) - 1))] = key;
+      f.count += __popcll(join);
     }
   }
 }
@@ -89,77 +164,135 @@ struct SelectArgs {
   int R, W, V, eos, pad, splits, span;  // span: elements per split
   float* cand_v;  // [R W, splits, W]
   int32_t* cand_i;
-  float2* norm;  // [R W, splits]: reference maximum, sum
+  float2* norm;  // [R W, splits]: largest logit, sum of exponentials against it
 };
 
-// one workgroup per (row, split)
+template <int DT>
+__device__ inline void unpack(const mf::u4& w, float* x) {
+#pragma unroll
+  for (int e = 0; e < (DT == UC_F32 ? 4 : 8); ++e) {
+    if constexpr (DT == UC_F32) x[e] = __uint_as_float(w[e]);
+    else if constexpr (DT == UC_BF16) x[e] = __uint_as_float(e & 1 ? w[e / 2] & 0xFFFF0000u : w[e / 2] << 16);
+    else x[e] = f16_to_f32((uint16_t)(w[e / 2] >> (16 * (e & 1))));
+  }
+}
+
+// One workgroup per (row, split); its waves take the vectors of the split in
+// turn, the next one's load under way.
 template <int DT>
 __global__ __launch_bounds__(256) void beam_rows_kernel(SelectArgs a) {
   constexpr int N = DT == UC_F32 ? 4 : 8;
   constexpr int EB = DT == UC_F32 ? 4 : 2;
   const int row = blockIdx.x / a.splits, split = blockIdx.x % a.splits;
   if (a.done && a.done[row]) return;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, W = a.W;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), W = a.W;
   const char* p = (const char*)a.logits + (int64_t)row * a.ld * EB;
   const int first = split * a.span, end = min(a.V, first + a.span);
   // whole 16-byte vectors from `from` on; single elements before and behind
   const int from = min(end, first + (int)(((16 - ((uintptr_t)(p + (int64_t)first * EB) & 15)) & 15) / EB));
   const int vecs = (end - from) / N, to = from + vecs * N;
-  Best b{-INFINITY, INT32_MAX, -INFINITY, INT32_MAX};
-  float m = -INFINITY, s = 0.0f;
-  {
-    const int n_head = from - first, n_edge = n_head + end - to;  // at most 14, one per lane of wave 0
-    float x[1] = {-INFINITY};
-    int at = 0;
-    const bool in = wave == 0 && lane < n_edge;
-    if (in) {
-      at = lane < n_head ? first + lane : to + lane - n_head;
-      x[0] = elem<DT>(p, at);
-    }
-    consume<1>(x, at, in, W, lane, b, m, s);
-  }
-  const char* vec = p + (int64_t)from * EB;
-  for (int i = threadIdx.x; i - lane < vecs; i += 256) {
-    float x[N];
-    const bool in = i < vecs;
-    mf::u4 w = mf::u4{0, 0, 0, 0};
-    if (in) w = __builtin_nontemporal_load(reinterpret_cast<const mf::u4*>(vec) + i);
+  __shared__ uint64_t gathered[4][kCap];
+  uint64_t* g = gathered[wave];
+  Floor f{-INFINITY, 0, 0};
+  float s = 0.0f;
+  const mf::u4* vec = reinterpret_cast<const mf::u4*>(p + (int64_t)from * EB);
+  constexpr int DEPTH = 4;  // vectors of a lane under way
+  mf::u4 w[DEPTH];
+  int i = threadIdx.x;
+  // loads without branches (past the end: the last vector again), so that
+  // waiting for one leaves the others under way
+  const int last = max(vecs - 1, 0);
+  auto load = [&](int at) { return __builtin_nontemporal_load(vec + min(at, last)); };
+  if (vecs > 0) {
 #pragma unroll
-    for (int e = 0; e < N; ++e) {
-      float f;
-      if constexpr (DT == UC_F32) f = __uint_as_float(w[e]);
-      else if constexpr (DT == UC_BF16) f = __uint_as_float(e & 1 ? w[e / 2] & 0xFFFF0000u : w[e / 2] << 16);
-      else f = f16_to_f32((uint16_t)(w[e / 2] >> (16 * (e & 1))));
-      x[e] = in ? fmaxf(f, -INFINITY) : -INFINITY;
+    for (int k = 0; k < DEPTH; ++k) w[k] = load(i + k * 256);
+  }
+  // W of the 256 lanes' maxima over their first vectors reach the least of the
+  // four waves' (W/4)-th largest ones, so nothing below it is gathered: of
+  // 8192 elements of one kind about W pass.
+  __shared__ float s_nth[4], s_max[4];
+  float r;
+  {
+    float mx = -INFINITY;
+#pragma unroll
+    for (int k = 0; k < DEPTH; ++k)
+      if (i + k * 256 < vecs) {
+        float x[N];
+        unpack<DT>(w[k], x);
+#pragma unroll
+        for (int e = 0; e < N; ++e) mx = fmaxf(mx, x[e]);
+      }
+    const float most = max_of_wave(mx), nth = nth_largest(mx, (W + 3) / 4, lane);
+    if (lane == 0) s_max[wave] = most, s_nth[wave] = nth;
+    __syncthreads();
+    f.v = fminf(fminf(s_nth[0], s_nth[1]), fminf(s_nth[2], s_nth[3]));
+    f.key = key_of(f.v, INT32_MAX) - 1;  // one of this value joins, whatever its index
+    r = held(fmaxf(fmaxf(s_max[0], s_max[1]), fmaxf(s_max[2], s_max[3]))) * kLog2e;
+  }
+  for (int done = 0; done < vecs; done += DEPTH * 256) {
+#pragma unroll
+    for (int k = 0; k < DEPTH; ++k, i += 256) {
+      float x[N];
+      unpack<DT>(w[k], x);
+      w[k] = load(i + DEPTH * 256);
+      consume<N>(x, from + i * N, i < vecs, W, lane, g, f, r, s);
     }
-    consume<N>(x, from + i * N, in ? N : 0, W, lane, b, m, s);
+  }
+  if (wave == 3) {  // at most 14 elements beside the vectors, one per lane
+    const int n_head = from - first, n_edge = n_head + end - to;
+    const bool in = lane < n_edge;
+    const int at = in ? (lane < n_head ? first + lane : to + lane - n_head) : 0;
+    float x[1] = {in ? load_elem(p, DT, at) : -INFINITY};
+    consume<1>(x, at, in, W, lane, g, f, r, s);
   }
   // the wave's sum, then the workgroup's lists and sums
-  const float mw = wave_max(m);
-  s = wave_sum(m == -INFINITY ? 0.0f : s * exp2f((m - mw) * kLog2e));
-  __shared__ float lv[4 * kMaxW], lm[4], ls[4];
-  __shared__ int li[4 * kMaxW];
-  if (lane < W) {
-    lv[wave * W + lane] = b.v;
-    li[wave * W + lane] = b.i;
-  }
-  if (lane == 0) lm[wave] = mw, ls[wave] = s;
+  s = wave_sum(s);
+  __shared__ float ls[4];
+  __shared__ int counts[4];
+  __shared__ float s_best;
+  if (lane == 0) ls[wave] = s, counts[wave] = f.count;
+  if (threadIdx.x == 0) s_best = -INFINITY;
   __syncthreads();
+  // an element's rank is the number of those before it
   const int64_t out = (int64_t)blockIdx.x * W;
-  if ((int)threadIdx.x < 4 * W) {
-    const float v = lv[threadIdx.x];
-    const int i = li[threadIdx.x];
+  const int c1 = counts[0], c2 = c1 + counts[1], c3 = c2 + counts[2], n = c3 + counts[3];
+  for (int t = threadIdx.x; t - lane < n; t += 256) {
+    const int h = (t >= c1) + (t >= c2) + (t >= c3), at = t - (h == 0 ? 0 : h == 1 ? c1 : h == 2 ? c2 : c3);
+    const uint64_t key = t < n ? gathered[h][at] : 0;
     int rank = 0;
-    for (int k = 0; k < 4 * W; ++k)
-      rank += before(lv[k], li[k], v, i) || (lv[k] == v && li[k] == i && k < (int)threadIdx.x);
-    if (rank < W) a.cand_v[out + rank] = v, a.cand_i[out + rank] = i;
+    for (int k = 0; k < 4; ++k) {
+      const int count = counts[k];
+#pragma unroll 4
+      for (int j = 0; j < count; ++j) rank += gathered[k][j] > key;
+    }
+    if (t < n && rank < W) {
+      a.cand_v[out + rank] = value_of(key);
+      a.cand_i[out + rank] = index_of(key);
+      if (rank == 0) s_best = value_of(key);
+    }
   }
-  if (threadIdx.x == 0) {
-    const float M = fmaxf(fmaxf(lm[0], lm[1]), fmaxf(lm[2], lm[3]));
-    float sum = 0.0f;
-    for (int k = 0; k < 4; ++k) sum += lm[k] == -INFINITY ? 0.0f : ls[k] * exp2f((lm[k] - M) * kLog2e);
-    a.norm[blockIdx.x] = float2{M, sum};
+  if ((int)threadIdx.x >= n && (int)threadIdx.x < W) {  // a split of fewer elements
+    a.cand_v[out + threadIdx.x] = -INFINITY;
+    a.cand_i[out + threadIdx.x] = INT32_MAX;
   }
+  __syncthreads();
+  // the split's largest logit (none: -inf), and the sum of exp(x - it)
+  const float top = s_best;
+  float sum = ((ls[0] + ls[1]) + (ls[2] + ls[3])) * exp2f(-fmaf(top, kLog2e, -r));
+  const bool fits = top >= -kHeld && top <= kHeld && sum >= 1e-6f && sum < INFINITY;  // (at least 1, but for rounding)
+  if (!fits && top > -INFINITY && top < INFINITY) {
+    sum = 0.0f;
+    for (int k = first + threadIdx.x; k < end; k += 256) {
+      const float x = load_elem(p, DT, k);
+      sum += x == x ? exp2f((x - top) * kLog2e) : 0.0f;
+    }
+    sum = wave_sum(sum);
+    __syncthreads();
+    if (lane == 0) ls[wave] = sum;
+    __syncthreads();
+    sum = (ls[0] + ls[1]) + (ls[2] + ls[3]);
+  }
+  if (threadIdx.x == 0) a.norm[blockIdx.x] = float2{top, sum};
 }
 
 struct Total {
@@ -167,87 +300,142 @@ struct Total {
   int flat;
 };
 __device__ inline bool before(const Total& x, const Total& y) { return x.v > y.v || (x.v == y.v && x.flat < y.flat); }
+struct FirstStep {  // the total that comes first
+  Total& t;
+  template <int CTRL, int ROWS>
+  __device__ void step() {
+    const uint64_t u = (uint64_t)__double_as_longlong(t.v);
+    const uint32_t lo = dpp<CTRL, ROWS>((uint32_t)u, (uint32_t)u), hi = dpp<CTRL, ROWS>(u >> 32, u >> 32);
+    const Total y{__longlong_as_double((int64_t)((uint64_t)hi << 32 | lo)), (int)dpp<CTRL, ROWS>(t.flat, t.flat)};
+    if (before(y, t)) t = y;
+  }
+};
 
-// one workgroup per request: totals of the candidates, W rounds of the best
+// One workgroup per request: totals of the candidates in registers (at most
+// kPer of a thread, by the choice of splits), then W rounds of the first among
+// them.
+constexpr int kMostPer = 16, kMaxRows = 512;  // splits of a request: W min(64, 4096 / W^2)
+template <int kPer>
 __global__ __launch_bounds__(256) void beam_pick_kernel(SelectArgs a) {
-  __shared__ double top[kMaxW], log_sum[kMaxW];  // a beam's largest logit, and the log of its sum of exponentials
-  __shared__ Total best[4];
+  __shared__ double log_sum[kMaxW];  // of a beam's exponentials against its largest logit
+  __shared__ float top[kMaxW];
+  __shared__ Total best[2][4];
   __shared__ float score[kMaxW];  // read whole first: the outputs may be the inputs
   __shared__ bool ended[kMaxW];
-  const int r = blockIdx.x, W = a.W, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  for (int b = wave; b < W; b += 4) {  // a wave per beam; splits <= 64
-    const int64_t row = (int64_t)r * W + b;
-    const bool gone = a.done && a.done[row];
-    double M = 0.0, z = 0.0;
-    if (!gone) {
-      const float2 n = lane < a.splits ? a.norm[row * a.splits + lane] : float2{-INFINITY, 0.0f};
-      M = wave_max(n.x);
-      const double part = n.x == -INFINITY ? 0.0 : (double)n.y * exp((double)n.x - M);
-      z = log(wave_sum_d(part));  // not finite if no logit is, or one is +inf
-    }
-    if (lane == 0) {
-      top[b] = M;
-      log_sum[b] = z;
-      score[b] = a.score[row];
-      ended[b] = gone;
+  const int q = blockIdx.x, W = a.W, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int per = a.splits * W, n = W * per;  // candidate c: beam c / per
+  int ci[kPer];
+  float cv[kPer];
+#pragma unroll
+  for (int k = 0; k < kPer; ++k) {
+    const int c = threadIdx.x + k * 256;
+    ci[k] = INT32_MAX;
+    cv[k] = -INFINITY;
+    if (k * 256 < n && c < n) {  // (an ended beam's are not written; not used either)
+      ci[k] = a.cand_i[(int64_t)q * n + c];
+      cv[k] = a.cand_v[(int64_t)q * n + c];
     }
   }
+  __shared__ float2 norm[kMaxRows];
+  for (int i = threadIdx.x; i < W * a.splits; i += 256) norm[i] = a.norm[(int64_t)q * W * a.splits + i];
   __syncthreads();
-  // candidate c of the request: beam c / (splits W)
-  const int per = a.splits * W, n = W * per;
-  auto total = [&](int c) {
-    const int b = c / per, k = c % per;
-    const int64_t row = (int64_t)r * W + b;
-    const double sc = score[b];
-    Total t{-INFINITY, INT32_MAX};
-    const bool gone = ended[b];
-    const double base = sc - log_sum[b];
-    if (gone || !(base > -INFINITY && base < INFINITY)) {
-      // an ended beam goes on by its pad token alone; one whose totals are
-      // all -inf offers its first tokens
-      if (k < W) {
-        int tok = k;
-        if (gone && k == 0) tok = a.pad, t.v = sc > -INFINITY && sc < INFINITY ? sc : -INFINITY;
-        else if (gone) tok = k - 1 < a.pad ? k - 1 : k;
-        if (tok < a.V) t.flat = b * a.V + tok;
+  if ((int)threadIdx.x < W) {  // a lane per beam
+    const int b = threadIdx.x;
+    const int64_t row = (int64_t)q * W + b;
+    const bool gone = a.done && a.done[row];
+    double z = 0.0;
+    float t = -INFINITY;
+    if (!gone) {
+      for (int k = 0; k < a.splits; ++k) t = fmaxf(t, norm[b * a.splits + k].x);
+      // a beam without a finite logit, or with one of +inf, has no totals
+      const bool some = t > -INFINITY && t < INFINITY;
+      for (int k = 0; k < a.splits; ++k) {
+        const float2 x = norm[b * a.splits + k];
+        if (some && x.x > -INFINITY) z += (double)x.y * (double)exp2f((x.x - t) * kLog2e);
       }
-      return t;
+      z = some ? log(z) : INFINITY;
     }
-    const int i = a.cand_i[row * per + k];
-    if (i == INT32_MAX) return t;
-    t.v = base + ((double)a.cand_v[row * per + k] - top[b]);
-    t.flat = b * a.V + i;
-    return t;
+    log_sum[b] = z;
+    top[b] = t;
+    score[b] = a.score[row];
+    ended[b] = gone;
+  }
+  __syncthreads();
+  double tv[kPer];
+#pragma unroll
+  for (int k = 0; k < kPer; ++k) {
+    tv[k] = -INFINITY;
+    const int c = threadIdx.x + k * 256;
+    if (k * 256 >= n || c >= n) {
+      ci[k] = INT32_MAX;
+      continue;
+    }
+    const int b = c / per, j = c % per;
+    const double sc = score[b], base = sc - log_sum[b];
+    if (ended[b] || !(base > -INFINITY && base < INFINITY)) {
+      // an ended beam goes on by its pad token alone; one without totals
+      // offers its first tokens
+      int tok = j < W ? j : a.V;
+      if (ended[b] && j == 0) tok = a.pad, tv[k] = sc > -INFINITY && sc < INFINITY ? sc : -INFINITY;
+      else if (ended[b] && j < W) tok = j - 1 < a.pad ? j - 1 : j;
+      ci[k] = tok < a.V ? b * a.V + tok : INT32_MAX;
+    } else if (ci[k] != INT32_MAX) {
+      tv[k] = base + ((double)cv[k] - (double)top[b]);
+      ci[k] += b * a.V;
+    }
+  }
+  auto write = [&](int k, const Total& t) {
+    const int b = t.flat / a.V, tok = t.flat % a.V;
+    const int64_t to = (int64_t)q * W + k;
+    a.score_out[to] = (float)t.v;
+    a.parent[to] = b;
+    a.token[to] = tok;
+    if (a.done_out) a.done_out[to] = ended[b] || tok == a.eos;
   };
-  Total last{INFINITY, -1};  // the one chosen before
+  if constexpr (kPer == 1) {  // one wave takes them all: no barriers
+    __shared__ Total all[256];
+    all[threadIdx.x] = Total{tv[0], ci[0]};
+    __syncthreads();
+    if (wave) return;
+    Total c[4], chosen{-INFINITY, INT32_MAX};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) c[j] = all[lane + 64 * j];
+    for (int k = 0; k < W; ++k) {
+      Total t = c[0];
+#pragma unroll
+      for (int j = 1; j < 4; ++j)
+        if (before(c[j], t)) t = c[j];
+      wave_fold(FirstStep{t});
+      const uint64_t u = (uint64_t)__double_as_longlong(t.v);
+      const uint64_t v = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(u >> 32), 63) << 32 |
+                         (uint32_t)__builtin_amdgcn_readlane((int)u, 63);
+      t = Total{__longlong_as_double((int64_t)v), __builtin_amdgcn_readlane(t.flat, 63)};
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (c[j].flat == t.flat) c[j] = Total{-INFINITY, INT32_MAX};
+      if (lane == k) chosen = t;
+    }
+    if (lane < W) write(lane, chosen);
+    return;
+  }
   for (int k = 0; k < W; ++k) {
     Total t{-INFINITY, INT32_MAX};
-    for (int c = threadIdx.x; c < n; c += 256) {
-      const Total x = total(c);
-      if (before(last, x) && before(x, t)) t = x;
-    }
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) {
-      Total y;
-      y.v = __shfl_xor(t.v, o, 64);
-      y.flat = __shfl_xor(t.flat, o, 64);
-      if (before(y, t)) t = y;
+    for (int j = 0; j < kPer; ++j) {
+      const Total x{tv[j], ci[j]};
+      if (before(x, t)) t = x;
     }
-    if (lane == 0) best[wave] = t;
+    wave_fold(FirstStep{t});
+    if (lane == 63) best[k & 1][wave] = t;
     __syncthreads();
-    t = best[0];
+    t = best[k & 1][0];
+#pragma unroll
     for (int i = 1; i < 4; ++i)
-      if (before(best[i], t)) t = best[i];
-    __syncthreads();
-    last = t;
-    if (threadIdx.x == 0) {
-      const int b = t.flat / a.V, tok = t.flat % a.V;
-      const int64_t to = (int64_t)r * W + k;
-      a.score_out[to] = (float)t.v;
-      a.parent[to] = b;
-      a.token[to] = tok;
-      if (a.done_out) a.done_out[to] = ended[b] || tok == a.eos;
-    }
+      if (before(best[k & 1][i], t)) t = best[k & 1][i];
+#pragma unroll
+    for (int j = 0; j < kPer; ++j)
+      if (ci[j] == t.flat) tv[j] = -INFINITY, ci[j] = INT32_MAX;
+    if (threadIdx.x == 0) write(k, t);
   }
 }
 
@@ -271,20 +459,23 @@ template <int MAXW>
 __global__ __launch_bounds__(256) void beam_reorder_kernel(ReorderArgs a) {
   __shared__ int s_from[kMaxW], s_last[kMaxW];  // a row's parent, and the row whose last page it takes (-1: its parent's)
   const int r = blockIdx.x, W = a.W;
-  if (threadIdx.x == 0) {
+  if (threadIdx.x < 64) {  // a lane per beam
+    const int b = threadIdx.x;
+    const int p = b < W ? min(max(a.parent[(int64_t)r * W + b], 0), W - 1) : -1;
     uint32_t has = 0;  // beams with a child
-    for (int b = 0; b < W; ++b) {
-      const int p = min(max(a.parent[(int64_t)r * W + b], 0), W - 1);
-      s_from[b] = p;
-      s_last[b] = has >> p & 1 ? -2 : -1;
-      has |= 1u << p;
+    bool again = false;
+    for (int j = 0; j < W; ++j) {
+      const int pj = __builtin_amdgcn_readlane(p, j);
+      has |= 1u << pj;
+      again |= j < b && pj == p;
     }
-    uint32_t free = ~has & (W == 32 ? ~0u : (1u << W) - 1);
-    for (int b = 0; b < W; ++b)
-      if (s_last[b] == -2) {
-        s_last[b] = __ffs(free) - 1;
-        free &= free - 1;
-      }
+    const uint64_t extra = __builtin_amdgcn_ballot_w64(b < W && again);
+    if (b < W) {
+      uint32_t free = ~has & (W == 32 ? ~0u : (1u << W) - 1);
+      for (int k = __popcll(extra & ((1ull << b) - 1)); k > 0; --k) free &= free - 1;
+      s_from[b] = p;
+      s_last[b] = again ? __ffs(free) - 1 : -1;
+    }
   }
   __syncthreads();
   if ((int)blockIdx.y < a.table_blocks) {
@@ -341,10 +532,11 @@ __global__ __launch_bounds__(256) void beam_reorder_kernel(ReorderArgs a) {
 }
 
 // Splits of a row: about four workgroups per CU over all rows, a span of at
-// least 4096 elements (a workgroup's fixed work is a few microseconds).
+// least 2048 elements (a workgroup's fixed work is a few microseconds), and
+// candidates that the second kernel holds in registers.
 int beam_splits(int R, int W, int V) {
   const int want = (4 * device_cus() + R * W - 1) / (R * W);
-  return max(1, min(min(want, 64), V / 4096));
+  return max(1, min(min(want, min(64, 256 * kMostPer / (W * W))), V / 2048));
 }
 size_t align_up(size_t x) { return (x + 255) & ~(size_t)255; }
 
@@ -367,7 +559,10 @@ hipError_t launch_beam_select(const void* logits, int dt, int64_t ld, const floa
   if (dt == UC_BF16) hipLaunchKernelGGL(beam_rows_kernel<UC_BF16>, dim3(rows), dim3(256), 0, st, a);
   else if (dt == UC_F16) hipLaunchKernelGGL(beam_rows_kernel<UC_F16>, dim3(rows), dim3(256), 0, st, a);
   else hipLaunchKernelGGL(beam_rows_kernel<UC_F32>, dim3(rows), dim3(256), 0, st, a);
-  hipLaunchKernelGGL(beam_pick_kernel, dim3(R), dim3(256), 0, st, a);
+  const int per = (W * W * splits + 255) / 256;
+  if (per == 1) hipLaunchKernelGGL(beam_pick_kernel<1>, dim3(R), dim3(256), 0, st, a);
+  else if (per <= 4) hipLaunchKernelGGL(beam_pick_kernel<4>, dim3(R), dim3(256), 0, st, a);
+  else hipLaunchKernelGGL(beam_pick_kernel<kMostPer>, dim3(R), dim3(256), 0, st, a);
   return hipGetLastError();
 }
 
