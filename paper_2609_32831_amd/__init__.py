@@ -534,7 +534,7 @@ class PageCache:
         assert scale_k.shape[:3] == codes_k.shape[:3]
         self.n_pages, self.Hkv, self.page_rows, self.D = n_pages, Hkv, P, 2 * half
         self.group = self.D // scale_k.shape[3]
-        self.device = codes_k.device
+        self.device, self.at = codes_k.device, codes_k.get_device()
         self.t = {"codes_k": codes_k, "codes_v": codes_v, "scale_k": scale_k, "scale_v": scale_v}
         self.desc = uc_page_cache(n_pages=n_pages, page_rows=P, Hkv=Hkv, D=self.D,
                                   group=self.group, codes_k=codes_k.data_ptr(),
@@ -553,27 +553,30 @@ def page_cache(n_pages: int, page_rows: int, Hkv: int, D: int, group: int = 64,
     return PageCache(*codes, *words)
 
 
-def _ints(*ts: Optional[torch.Tensor]):
-    """Device int32 tensors, contiguous, as the paged calls take them."""
+def _ints(at: int, *ts: Optional[torch.Tensor]):
+    """Device int32 tensors, contiguous, on GPU `at`, as the paged calls take
+    them."""
     for t in ts:
-        assert t is None or (t.dtype == torch.int32 and t.is_contiguous()), "int32, contiguous"
-    first = ts[0]
-    assert all(t is None or t.device == first.device for t in ts), "tensors on several devices"
+        assert t is None or (t.dtype is torch.int32 and t.is_contiguous() and
+                             t.get_device() == at), "int32, contiguous, on one device"
 
 
-def _token_rows(x: torch.Tensor, heads: int, D: int) -> int:
-    """x [T, heads, D] with the heads of a token together; the distance of two
-    tokens in elements."""
-    assert x.dim() == 3 and x.shape[1] == heads and x.shape[2] == D, tuple(x.shape)
-    assert x.stride(2) == 1 and (heads == 1 or x.stride(1) == D), "a token's heads lie together"
-    return x.stride(0) if x.shape[0] > 1 else heads * D
+def _token_rows(x: torch.Tensor, y: torch.Tensor, T: int, heads: int, D: int) -> int:
+    """x and y [T, heads, D] with the heads of a token together, alike in
+    everything; the distance of two tokens in elements."""
+    sx = x.stride()
+    assert x.shape == (T, heads, D) and sx[2] == 1 and (heads == 1 or sx[1] == D), \
+        "[T, heads, D], a token's heads together"
+    assert x is y or (y.shape == x.shape and y.stride() == sx and y.dtype is x.dtype and
+                      y.get_device() == x.get_device()), "keys and values differ in their layout"
+    return sx[0] if T > 1 else heads * D
 
 
 def uc_page_free(table: torch.Tensor, len: torch.Tensor, page_rows: int, free_list: torch.Tensor,
                  pool: torch.Tensor, ws: Optional[torch.Tensor] = None, stream=None):
     """The pages that no sequence of table [S, nb] / len [S] holds: free_list
     [n_pages], pool [2] = (0, their count)."""
-    _ints(table, len, free_list, pool)
+    _ints(table.get_device(), table, len, free_list, pool)
     S, nb = table.shape
     n_pages = free_list.numel()
     assert len.numel() == S and pool.numel() == 2
@@ -591,11 +594,12 @@ def uc_page_step(len: torch.Tensor, new_len: torch.Tensor, table: torch.Tensor, 
     """One step's pages and slots: table [S, nb] gains the new pages' entries,
     len_out [S], q_start [S + 1], slots [n_slots], pool_out [2] and refused
     [S] (uint8) are written."""
-    _ints(table, len, new_len, free_list, pool, len_out, q_start, slots, pool_out)
+    at = table.get_device()
+    _ints(at, table, len, new_len, free_list, pool, len_out, q_start, slots, pool_out)
     S, nb = table.shape
     assert len.numel() == new_len.numel() == len_out.numel() == refused.numel() == S
     assert q_start.numel() == S + 1 and pool.numel() == pool_out.numel() == 2
-    assert refused.dtype == torch.uint8 and refused.is_contiguous()
+    assert refused.dtype is torch.uint8 and refused.is_contiguous() and refused.get_device() == at
     _check(lib.uc_page_step(S, page_rows, free_list.numel(), len.data_ptr(), new_len.data_ptr(),
                             table.data_ptr(), nb, free_list.data_ptr(), pool.data_ptr(),
                             len_out.data_ptr(), q_start.data_ptr(), slots.data_ptr(),
@@ -607,12 +611,10 @@ def uc_page_append(cache: PageCache, k_new: torch.Tensor, v_new: torch.Tensor,
                    slots: torch.Tensor, copies: Optional[torch.Tensor] = None, stream=None):
     """Quantise k_new / v_new [T, Hkv, D] into slots [T]; copies [n, 3] as
     uc_beam_reorder writes them."""
-    _ints(slots, copies)
+    _ints(cache.at, slots, copies)
     T = slots.numel()
-    assert k_new.shape == v_new.shape and k_new.dtype == v_new.dtype and k_new.shape[0] == T
-    ld = _token_rows(k_new, cache.Hkv, cache.D)
-    assert _token_rows(v_new, cache.Hkv, cache.D) == ld, "k_new and v_new differ in their strides"
-    assert k_new.device == v_new.device == slots.device == cache.device
+    ld = _token_rows(k_new, v_new, T, cache.Hkv, cache.D)
+    assert k_new.get_device() == cache.at, "on the cache's device"
     _check(lib.uc_page_append(cache._ref, k_new.data_ptr(), v_new.data_ptr(),
                               TORCH_DT[k_new.dtype], ld, T, slots.data_ptr(), _ptr(copies),
                               0 if copies is None else copies.numel() // 3, _stream(stream)),
@@ -622,12 +624,10 @@ def uc_page_append(cache: PageCache, k_new: torch.Tensor, v_new: torch.Tensor,
 def uc_page_read(cache: PageCache, slots: torch.Tensor, k_out: torch.Tensor, v_out: torch.Tensor,
                  stream=None):
     """The values held in slots [T] -> k_out / v_out [T, Hkv, D]."""
-    _ints(slots)
+    _ints(cache.at, slots)
     T = slots.numel()
-    assert k_out.shape == v_out.shape and k_out.dtype == v_out.dtype and k_out.shape[0] == T
-    ld = _token_rows(k_out, cache.Hkv, cache.D)
-    assert _token_rows(v_out, cache.Hkv, cache.D) == ld, "k_out and v_out differ in their strides"
-    assert k_out.device == v_out.device == slots.device == cache.device
+    ld = _token_rows(k_out, v_out, T, cache.Hkv, cache.D)
+    assert k_out.get_device() == cache.at, "on the cache's device"
     _check(lib.uc_page_read(cache._ref, slots.data_ptr(), T, k_out.data_ptr(), v_out.data_ptr(),
                             TORCH_DT[k_out.dtype], ld, _stream(stream)), "uc_page_read")
 
@@ -643,15 +643,16 @@ def uc_page_attend(cache: PageCache, q: torch.Tensor, q_start: torch.Tensor, len
     """Causal attention of the ragged tokens q [T, Hq, D] (sequence s: tokens
     q_start[s] .. q_start[s + 1] - 1, the last ones of its len[s] rows) over
     the cache's pages, into o [T, Hq, D] (q's dtype) and lse [T, Hq]."""
-    _ints(table, q_start, len)
+    at = cache.at
+    _ints(at, table, q_start, len)
     S, nb = table.shape
-    T, Hq, D = q.shape
+    T, Hq, _ = q.shape
+    ld = _token_rows(q, q, T, Hq, cache.D)
     assert len.numel() == S and q_start.numel() == S + 1
-    assert o.shape == q.shape and o.dtype == q.dtype and o.is_contiguous()
-    assert lse is None or (lse.dtype == torch.float32 and lse.is_contiguous() and
-                           lse.numel() == T * Hq)
-    assert q.device == o.device == table.device == cache.device
-    ld = _token_rows(q, Hq, cache.D)
+    assert o.shape == q.shape and o.dtype is q.dtype and o.is_contiguous()
+    assert lse is None or (lse.dtype is torch.float32 and lse.is_contiguous() and
+                           lse.numel() == T * Hq and lse.get_device() == at)
+    assert q.get_device() == o.get_device() == at, "on the cache's device"
     if ws is None:
         ws = _ws(lib.uc_page_attend_workspace_size(cache._ref, Hq, T, S, max_q), q.device)
     _check(lib.uc_page_attend(cache._ref, Hq, q.data_ptr(), TORCH_DT[q.dtype], ld, T, S, max_q,
@@ -672,13 +673,17 @@ def uc_beam_select(logits: torch.Tensor, score: torch.Tensor, done: Optional[tor
     """The W best continuations of every request: logits [R, W, V] (rows at
     one distance), score [R, W] float, done [R, W] uint8 or None."""
     R, W, V = logits.shape
-    assert logits.stride(2) == 1 and (R == 1 or logits.stride(0) == W * logits.stride(1))
-    ld = logits.stride(1) if W > 1 else max(logits.stride(0) if R > 1 else V, V)
-    _ints(parent, token)
-    for t, dt in ((score, torch.float32), (score_out, torch.float32), (parent, torch.int32),
-                  (token, torch.int32), (done, torch.uint8), (done_out, torch.uint8)):
-        assert t is None or (t.dtype == dt and t.is_contiguous() and t.numel() == R * W and
-                             t.device == logits.device)
+    s = logits.stride()
+    assert s[2] == 1 and (R == 1 or s[0] == W * s[1]), "rows of logits at one distance"
+    ld = s[1] if W > 1 else s[0] if R > 1 else V
+    at, n = logits.get_device(), R * W
+    _ints(at, parent, token)
+    for t in (score, score_out):
+        assert t.dtype is torch.float32 and t.is_contiguous() and t.get_device() == at
+    for t in (done, done_out):
+        assert t is None or (t.dtype is torch.uint8 and t.is_contiguous() and t.numel() == n and
+                             t.get_device() == at)
+    assert score.numel() == score_out.numel() == parent.numel() == token.numel() == n
     if ws is None:
         ws = _ws(lib.uc_beam_select_workspace_size(R, W, V), logits.device)
     _check(lib.uc_beam_select(R, W, V, logits.data_ptr(), TORCH_DT[logits.dtype], ld,
@@ -695,13 +700,14 @@ def uc_beam_reorder(parent: torch.Tensor, token: Optional[torch.Tensor], table: 
     columns are filled; token [R, W] joins them) to the beams' new places;
     copies [R * W, 3] for the next uc_page_append of every layer."""
     R, W = parent.shape
-    _ints(table, parent, token, len, table_out, copies, history, history_out)
-    assert table.shape[0] == R * W and table_out.shape == table.shape and len.numel() == R * W
-    assert copies.numel() == 3 * R * W and (token is None or token.numel() == R * W)
-    assert history is None or (history.shape[0] == R * W and history_out is not None and
+    n, nb = table.shape
+    _ints(table.get_device(), table, parent, token, len, table_out, copies, history, history_out)
+    assert n == R * W and table_out.shape == table.shape and len.numel() == n
+    assert copies.numel() == 3 * n and (token is None or token.numel() == n)
+    assert history is None or (history_out is not None and history.shape[0] == n and
                                history_out.shape == history.shape and token is not None)
-    _check(lib.uc_beam_reorder(R, W, parent.data_ptr(), _ptr(token), table.data_ptr(),
-                               table.shape[1], len.data_ptr(), page_rows, table_out.data_ptr(),
+    _check(lib.uc_beam_reorder(R, W, parent.data_ptr(), _ptr(token), table.data_ptr(), nb,
+                               len.data_ptr(), page_rows, table_out.data_ptr(),
                                copies.data_ptr(), _ptr(history), _ptr(history_out),
                                0 if history is None else history.shape[1], n_history,
                                _stream(stream)), "uc_beam_reorder")
