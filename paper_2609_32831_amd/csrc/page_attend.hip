@@ -24,6 +24,7 @@
 // workgroup; one cut into several leaves a record (m, l, o) per piece, merged
 // by a second kernel in the order of the pieces.
 #include <algorithm>
+#include <type_traits>
 
 #include "page_common.h"
 
@@ -579,31 +580,43 @@ __global__ __launch_bounds__(256, 2) void page_tokens_kernel(PageAttendArgs a, i
 }
 
 // ---------------------------------------------------------------- prompts
-// Blocks of 128 query rows of a KV head, each over the tiles that its last
-// row sees; the line is made of all blocks' tiles.  A workgroup's four waves
-// take 32 rows each and share the tile in LDS, where it stands as c * s in
-// bf16 (exact; the 4-bit rows are read and unpacked once per 128 rows); the
-// minima go through matrix instructions of their own,
-//   q . k += sum_g m_g sum(q_g),  o += sum_j p_j m_jg,
-// with sum(q_g) in three bf16 parts (24 bits).  Bound by the matrix and vector
-// units together: per 64 keys x 32 rows a wave issues 32 (QP 1) + 64 matrix
-// instructions of 16 cycles for the two products and 12 for the minima, and
-// about 500 vector instructions of 4 cycles (softmax, unpacking).
-constexpr int QROWS = 128;
+// Blocks of 32 query rows a wave, each over the tiles that its last row sees;
+// the line is made of all blocks' tiles.  A workgroup's waves share the tile
+// in LDS, where the 4-bit rows, read and unpacked once for all of them, stand
+// as fp16: with the power of two 2^e of the key's largest step taken out,
+// c * (s 2^-e) has 8 significant bits and is exact, and so is the minimum.
+// The powers return where they cost nothing: the keys' in the factor that
+// turns a product into a logit, the values' in the exponent,
+//   w_j = 2^(logit_j + e_j - m),  o ~ sum_j w_j (v_j 2^-e_j),  l = sum_j w_j 2^-e_j,
+// with the reference m kept over logit + e, so that w_j, rounded to fp16 (11
+// bits), is measured by what key j contributes whatever the values' sizes.  l
+// is summed in binary32 before that rounding.  Steps of values from 2^-60 to
+// 2^88 keep all their bits.  The minima go through matrix instructions of
+// their own, q . k += sum_g m_g sum(q_g) with sum(q_g) in three fp16 parts.
+// Queries enter as fp16 too, exactly (a row far from 1 by a power of two).
+//
+// Per 64 keys x 32 rows a wave issues 64 matrix instructions of 16 cycles for
+// the two products and 12 for the minima, and some 400 vector instructions of
+// 4 cycles; both bound it.
+template <int WV>
+constexpr int kQRows = 32 * WV;
 
 // blocks of a sequence in the prompt kernel
+template <int WV>
 __device__ inline int prompt_blocks(const Seq& x, int G) {
   const int64_t rows = (int64_t)x.n * G;
-  return rows <= 16 ? 0 : (int)((rows + QROWS - 1) / QROWS);
+  return rows <= 16 ? 0 : (int)((rows + kQRows<WV> - 1) / kQRows<WV>);
 }
 // tiles of its block b, at least one
+template <int WV>
 __device__ inline int prompt_tiles(const Seq& x, int G, int b) {
-  const int64_t last = min((int64_t)x.n - 1, ((int64_t)b * QROWS + QROWS - 1) / G);
+  const int64_t last = min((int64_t)x.n - 1, ((int64_t)b * kQRows<WV> + kQRows<WV> - 1) / G);
   const int64_t sees = max((int64_t)0, min((int64_t)x.len, (int64_t)x.len - x.n + last + 1));
   return tiles_of((int)sees);
 }
 
 // before[s]: units of the sequences ahead of s, before[S]: all of them
+template <int WV>
 __global__ __launch_bounds__(1024) void page_plan_kernel(PageAttendArgs a, int* __restrict__ before) {
   __shared__ int part[16];
   const int lane = threadIdx.x & 63;
@@ -612,7 +625,7 @@ __global__ __launch_bounds__(1024) void page_plan_kernel(PageAttendArgs a, int* 
     const int s = s0 + threadIdx.x;
     Seq x{0, 0, 0};
     if (s < a.S) x = seq_of(a, s);
-    const int blocks = prompt_blocks(x, a.G);
+    const int blocks = prompt_blocks<WV>(x, a.G);
     int mine = 0;
     // the wave counts one sequence after the other, a block per lane
     for (uint64_t todo = __builtin_amdgcn_ballot_w64(blocks > 0); todo; todo &= todo - 1) {
@@ -620,7 +633,7 @@ __global__ __launch_bounds__(1024) void page_plan_kernel(PageAttendArgs a, int* 
       const Seq y{0, __shfl(x.n, from, 64), __shfl(x.len, from, 64)};
       const int nb = __shfl(blocks, from, 64);
       int sum = 0;
-      for (int b = lane; b < nb; b += 64) sum += prompt_tiles(y, a.G, b);
+      for (int b = lane; b < nb; b += 64) sum += prompt_tiles<WV>(y, a.G, b);
 #pragma unroll
       for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
       if (lane == from) mine = sum;
@@ -636,38 +649,56 @@ __global__ __launch_bounds__(1024) void page_plan_kernel(PageAttendArgs a, int* 
 template <int D>
 constexpr int kRow = 2 * D + 32;  // bytes of a staged row: 8 consecutive rows start in different 8-bank groups
 
+typedef _Float16 half2 __attribute__((ext_vector_type(2)));
+
 template <int D>
-struct PromptLds {
-  uint8_t k[KT * kRow<D>];
+struct PromptTile {
+  uint8_t k[KT * kRow<D>];  // c * s 2^-e in fp16; of eight channels in the order 0 4 1 5 2 6 3 7
   uint8_t v[KT * kRow<D>];
-  uint16_t km[KT][8];      // minima of a key, zeros behind them
-  uint16_t vm[4][KT + 8];  // minima of a value group, by key
+  _Float16 km[KT][8];      // minima (2^-e) of a key, zeros behind them
+  _Float16 vm[4][KT + 8];  // minima (2^-e) of a value group, by key
+  float kf[KT];            // logit of a product: scale * 2^e
+  float ve[KT], vi[KT];    // e and 2^-e of the values
 };
 
-// a word's eight codes times s as bf16
-__device__ inline u4 times(uint32_t w, float s) {
-  const uint32_t m = opaque(0x0F0F0F0Fu);
-  const uint32_t lo = w & m, hi = (w >> 4) & m;
-  float x[8];
+// a word's eight codes times a step, as fp16: (1024 + c) s - 1024 s
+struct Unpack {
+  uint32_t mask, base;
+  __device__ Unpack() : mask(opaque(0x000F000Fu)), base(opaque(0x64006400u)) {}
+  __device__ u4 times(uint32_t w, half2 s, half2 off) const {
+    u4 r;
 #pragma unroll
-  for (int b = 0; b < 4; ++b) {
-    x[2 * b] = (float)((lo >> (8 * b)) & 0xFFu) * s;
-    x[2 * b + 1] = (float)((hi >> (8 * b)) & 0xFFu) * s;
+    for (int i = 0; i < 4; ++i) {
+      const half2 x = __builtin_bit_cast(half2, ((w >> (4 * i)) & mask) | base);
+      r[i] = __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(x, s, off));
+    }
+    return r;
   }
-  return u4{bf2(x[0], x[1]), bf2(x[2], x[3]), bf2(x[4], x[5]), bf2(x[6], x[7])};
+};
+
+// biased exponent of the power of two taken out of a row: its largest step
+// comes below 2 and its minima below 2^14
+template <int NG>
+__device__ inline int row_exponent(const uint32_t (&w)[NG], int least, int most) {
+  int e = 0;
+#pragma unroll
+  for (int n = 0; n < NG; ++n)
+    e = max(e, max((int)(w[n] >> 7 & 0xFF), (int)(w[n] >> 23 & 0xFF) - 12));
+  return e == 0 ? 127 : min(max(e, least), most);  // a row of zeros: any
 }
 
-template <int D, int NG, int QP>
-__global__ __launch_bounds__(256, 2) void page_prompt_kernel(PageAttendArgs a, int W_all,
-                                                             const int* __restrict__ units,
-                                                             float* __restrict__ rec, Cut* __restrict__ cuts) {
-  constexpr int KS = D / 32, DT = D / 16;
-  __shared__ __attribute__((aligned(16))) PromptLds<D> L;
+template <int D, int NG, int WV>
+__global__ __launch_bounds__(64 * WV, 2) void page_prompt_kernel(PageAttendArgs a, int W_all, bool q_f16,
+                                                                 const int* __restrict__ units,
+                                                                 float* __restrict__ rec, Cut* __restrict__ cuts) {
+  constexpr int KS = D / 32, DT = D / 16, QROWS = kQRows<WV>, THREADS = 64 * WV;
+  __shared__ __attribute__((aligned(16))) PromptTile<D> tiles_lds[2];
   __shared__ int s_part[16], s_block, s_before;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int i16 = lane & 15, g4 = lane >> 4;
   const int Hkv = a.pc.Hkv, h = blockIdx.x % Hkv, w = blockIdx.x / Hkv;
   const int G = a.G, Hq = G * Hkv, lgP = a.pc.lgP;
+  const Unpack unpack;
   if (threadIdx.x == 0) cuts[blockIdx.x] = Cut{-1, 0, 0, 0};
   const int U = units[a.S];
   if (U == 0) return;
@@ -682,13 +713,13 @@ __global__ __launch_bounds__(256, 2) void page_prompt_kernel(PageAttendArgs a, i
     else hi = mid;
   }
   Seq x = seq_of(a, s);
-  int nb = prompt_blocks(x, G);
+  int nb = prompt_blocks<WV>(x, G);
   if (threadIdx.x == 0) s_block = -1;
   {
     int base = units[s];
-    for (int b0 = 0; b0 < nb; b0 += 256) {
+    for (int b0 = 0; b0 < nb; b0 += THREADS) {
       const int b = b0 + threadIdx.x;
-      const int mine = b < nb ? prompt_tiles(x, G, b) : 0;
+      const int mine = b < nb ? prompt_tiles<WV>(x, G, b) : 0;
       int total;
       const int upto = base + block_scan(mine, s_part, total);
       if (upto - mine <= u0 && u0 < upto) {
@@ -699,63 +730,143 @@ __global__ __launch_bounds__(256, 2) void page_prompt_kernel(PageAttendArgs a, i
     }
   }
   // the slots behind a key's minima stay zero
-  for (int i = threadIdx.x; i < KT * 8; i += 256) (&L.km[0][0])[i] = 0;
+  for (int i = threadIdx.x; i < KT * 8; i += THREADS)
+    (&tiles_lds[0].km[0][0])[i] = (&tiles_lds[1].km[0][0])[i] = (_Float16)0.0f;
   __syncthreads();
   int b = s_block;
   if (b < 0) return;  // starts that overlap so often that the sums passed their type
   int before = s_before;
 
+  // A thread's share of a tile: 16 bytes of codes of a row of keys or values.
+  constexpr int CH = D / 32, TASKS = 2 * KT * CH, PER = TASKS > THREADS ? TASKS / THREADS : 1;
+  static_assert(PER <= 2, "one task of each kind at most");
+  u4 codes[PER];
+  uint32_t words[PER][NG];
+
   for (int u = u0; u < u1;) {
-    const int tiles = prompt_tiles(x, G, b);
+    const int tiles = prompt_tiles<WV>(x, G, b);
     const int t0 = u - before, t1 = min(tiles, u1 - before);
     const int rows = (int)min((int64_t)QROWS, (int64_t)x.n * G - (int64_t)b * QROWS);
     const int32_t* trow = a.table + (int64_t)s * a.ld;
+    bool bad = false;
 
-    u4 qb[2][QP][KS], sqb[2];
+    auto issue = [&](int t) {
+#pragma unroll
+      for (int i = 0; i < PER; ++i) {
+        const int task = threadIdx.x + i * THREADS, kind = task / (KT * CH), key = task % (KT * CH) / CH;
+        if (kind > 1) continue;
+        const int r = min(t * KT + key, x.len - 1), page = page_of(trow, r, lgP, a.pc.n_pages);
+        if (page < 0) bad = true;
+        const int64_t row = page_row(max(page, 0), Hkv, h, lgP, r);
+        codes[i] = *reinterpret_cast<const u4*>((kind ? a.pc.codes_v : a.pc.codes_k) + row * (D / 2) + task % CH * 16);
+        load_words<NG>((kind ? a.pc.scale_v : a.pc.scale_k) + row * NG, words[i]);
+      }
+    };
+    // the tile to LDS; rows past the sequence repeat its last one
+    auto stage = [&](PromptTile<D>& L) {
+#pragma unroll
+      for (int i = 0; i < PER; ++i) {
+        const int task = threadIdx.x + i * THREADS, kind = task / (KT * CH), key = task % (KT * CH) / CH, ch = task % CH;
+        if (kind > 1) continue;
+        const int E = kind ? row_exponent<NG>(words[i], 127 - 48, 127 + 76) : row_exponent<NG>(words[i], 24, 230);
+        const float out = __uint_as_float((uint32_t)(254 - E) << 23), in = __uint_as_float((uint32_t)E << 23);
+        half2 st[NG], off[NG];
+#pragma unroll
+        for (int n = 0; n < NG; ++n) {
+          const float f = word_step(words[i][n]) * out;
+          st[n] = __builtin_bit_cast(half2, h2(f, f));
+          off[n] = __builtin_bit_cast(half2, h2(-1024.0f * f, -1024.0f * f));
+        }
+        if (kind == 0) {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            // the word holds channels 32 step + 8 g ..
+            const int step = KS == 4 ? j : j % KS, g = (ch * 4 + j) / KS, n = step * NG / KS;
+            *reinterpret_cast<u4*>(L.k + key * kRow<D> + (step * 4 + g) * 16) = unpack.times(codes[i][j], st[n], off[n]);
+          }
+          if (ch == 0) {
+#pragma unroll
+            for (int n = 0; n < NG; ++n) L.km[key][n] = (_Float16)(word_min(words[i][n]) * out);
+            L.kf[key] = in * a.scale_log2;
+          }
+        } else {
+          half2 sv = st[0], ov = off[0];
+#pragma unroll
+          for (int n = 1; n < NG; ++n)
+            if (ch * NG / CH == n) sv = st[n], ov = off[n];
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            *reinterpret_cast<u4*>(L.v + key * kRow<D> + (ch * 4 + j) * 16) = unpack.times(codes[i][j], sv, ov);
+          if (ch == 0) {
+#pragma unroll
+            for (int n = 0; n < NG; ++n) L.vm[n][key] = (_Float16)(word_min(words[i][n]) * out);
+            L.ve[key] = (float)(E - 127);
+            L.vi[key] = out;
+          }
+        }
+      }
+    };
+    if (x.len > 0) issue(t0);
+
+    u4 qb[2][KS], sqb[2];
     int lim[2];
-    int64_t tok[2];  // the lane's query rows, among the rows of o
+    float qf[2];      // power of two taken out of the lane's query row
+    int64_t tok[2];   // the lane's query rows, among the rows of o
+    bool scaled = false;
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
       const int r = wave * 32 + c * 16 + i16;
-      const int rr = b * QROWS + min(r, rows - 1), i = rr / G, g = rr % G;
+      const int rr = b * QROWS + min(r, rows - 1), i = rr / G, gq = rr % G;
       lim[c] = (int)max((int64_t)0, min((int64_t)x.len, (int64_t)x.len - x.n + i + 1));
-      tok[c] = (int64_t)(x.q0 + i) * Hq + h * G + g;
-      const int64_t base = (int64_t)(x.q0 + i) * a.q_ld + (int64_t)(h * G + g) * D + g4 * 8;
-      float sq[NG];
-#pragma unroll
-      for (int g = 0; g < NG; ++g) sq[g] = 0.0f;
+      tok[c] = (int64_t)(x.q0 + i) * Hq + h * G + gq;
+      const int64_t base = (int64_t)(x.q0 + i) * a.q_ld + (int64_t)(h * G + gq) * D + g4 * 8;
+      float f[KS][8], most = 0.0f;
 #pragma unroll
       for (int t = 0; t < KS; ++t) {
         const u4 raw = *reinterpret_cast<const u4*>(static_cast<const uint16_t*>(a.q) + base + t * 32);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const float f0 = QP == 1 ? __uint_as_float(raw[e] << 16) : f16_to_f32((uint16_t)raw[e]);
-          const float f1 = QP == 1 ? __uint_as_float(raw[e] & 0xFFFF0000u) : f16_to_f32((uint16_t)(raw[e] >> 16));
-          sq[t * NG / KS] += f0 + f1;
-          if constexpr (QP == 1) {
-            qb[c][0][t][e] = raw[e];
-          } else {
-            const uint32_t hi = bf2(f0, f1);
-            qb[c][0][t][e] = hi;
-            qb[c][1][t][e] = bf2(f0 - __uint_as_float(hi << 16), f1 - __uint_as_float(hi & 0xFFFF0000u));
-          }
+          f[t][2 * e] = q_f16 ? f16_to_f32((uint16_t)raw[e]) : __uint_as_float(raw[e] << 16);
+          f[t][2 * e + 1] = q_f16 ? f16_to_f32((uint16_t)(raw[e] >> 16)) : __uint_as_float(raw[e] & 0xFFFF0000u);
+          most = fmaxf(most, fmaxf(fabsf(f[t][2 * e]), fabsf(f[t][2 * e + 1])));
         }
       }
-      // sums in three bf16 parts: part g4 in this lane's slots
+      most = fmaxf(most, __shfl_xor(most, 16, 64));
+      most = fmaxf(most, __shfl_xor(most, 32, 64));
+      const int E = (int)(__float_as_uint(most) >> 23);  // 2^(E - 127) <= most
+      const bool far = most > 0.0f && (E < 127 - 4 || E > 127 + 14);
+      const float out = far ? __uint_as_float((uint32_t)(254 - min(max(E, 1), 253)) << 23) : 1.0f;
+      qf[c] = far ? __uint_as_float((uint32_t)min(max(E, 1), 253) << 23) : 1.0f;
+      scaled |= far;
+      float sq[NG];
+#pragma unroll
+      for (int n = 0; n < NG; ++n) sq[n] = 0.0f;
+#pragma unroll
+      for (int t = 0; t < KS; ++t) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          f[t][e] *= out;
+          sq[t * NG / KS] += f[t][e];
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) qb[c][t][e] = h2(f[t][e], f[t][e + 4]);
+      }
+      // sums in three fp16 parts: part g4 in this lane's slots
       uint32_t bits[4] = {0, 0, 0, 0};
 #pragma unroll
-      for (int g = 0; g < NG; ++g) {
-        float y = sq[g];
+      for (int n = 0; n < NG; ++n) {
+        float y = sq[n];
         y += __shfl_xor(y, 16, 64);
         y += __shfl_xor(y, 32, 64);
 #pragma unroll
         for (int p = 0; p < 2; ++p)
-          if (p < g4) y -= bf16_to_f32(f32_to_bf16_bits(y));
-        const uint32_t v = g4 < 3 ? f32_to_bf16_bits(y) : 0;
-        bits[g >> 1] |= v << (16 * (g & 1));
+          if (p < g4) y -= f16_to_f32(f32_to_f16_bits(y));
+        const uint32_t v = g4 < 3 ? f32_to_f16_bits(y) : 0;
+        bits[n >> 1] |= v << (16 * (n & 1));
       }
       sqb[c] = u4{bits[0], bits[1], bits[2], bits[3]};
     }
+    scaled = __builtin_amdgcn_ballot_w64(scaled) != 0;
     const int lim_all = (int)max((int64_t)0, (int64_t)x.len - x.n + (int64_t)b * QROWS / G + 1);
 
     float m[2] = {kNone, kNone}, l[2] = {0.0f, 0.0f};
@@ -766,98 +877,66 @@ __global__ __launch_bounds__(256, 2) void page_prompt_kernel(PageAttendArgs a, i
 #pragma unroll
       for (int d = 0; d < DT; ++d) acc[c][d] = f4{0.f, 0.f, 0.f, 0.f};
     }
-    bool bad = false;
 
     if (x.len > 0) {
-      // a thread's share of a tile: 16 bytes of codes of a row, of keys and of
-      // values (D = 128), of one of them (D = 64)
-      constexpr int CH = D / 32;
-      const int key = D == 128 ? threadIdx.x >> 2 : (threadIdx.x & 127) >> 1, ch = threadIdx.x % CH;
-      const bool do_k = D == 128 || threadIdx.x < 128, do_v = D == 128 || threadIdx.x >= 128;
-      u4 ck, cv;
-      uint32_t wk[NG], wv[NG];
-      auto page_for = [&](int t) { return page_of(trow, min(t * KT + key, x.len - 1), lgP, a.pc.n_pages); };
-      auto issue = [&](int t, int page) {
-        if (page < 0) bad = true;
-        const int64_t row = page_row(max(page, 0), Hkv, h, lgP, min(t * KT + key, x.len - 1));
-        if (do_k) {
-          ck = *reinterpret_cast<const u4*>(a.pc.codes_k + row * (D / 2) + ch * 16);
-          load_words<NG>(a.pc.scale_k + row * NG, wk);
-        }
-        if (do_v) {
-          cv = *reinterpret_cast<const u4*>(a.pc.codes_v + row * (D / 2) + ch * 16);
-          load_words<NG>(a.pc.scale_v + row * NG, wv);
-        }
-      };
-      issue(t0, page_for(t0));
+      stage(tiles_lds[0]);
+      if (t0 + 1 < t1) issue(t0 + 1);
       for (int t = t0; t < t1; ++t) {
-        // stage the tile; rows past the sequence repeat its last one
-        if (do_k) {
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int wd = ch * 4 + i, step = wd % KS, g = wd / KS;  // channels 32 step + 8 g ..
-            float st = word_step(wk[0]);
-#pragma unroll
-            for (int n = 1; n < NG; ++n)
-              if (step * NG / KS == n) st = word_step(wk[n]);
-            *reinterpret_cast<u4*>(L.k + key * kRow<D> + (step * 4 + g) * 16) = times(ck[i], st);
-          }
-          if (ch == 0) {
-#pragma unroll
-            for (int n = 0; n < NG; ++n) L.km[key][n] = (uint16_t)(wk[n] >> 16);
-          }
-        }
-        if (do_v) {
-          float st = word_step(wv[0]);
-#pragma unroll
-          for (int n = 1; n < NG; ++n)
-            if (ch * NG / CH == n) st = word_step(wv[n]);
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            *reinterpret_cast<u4*>(L.v + key * kRow<D> + (ch * 4 + i) * 16) = times(cv[i], st);
-          if (ch == 0) {
-#pragma unroll
-            for (int n = 0; n < NG; ++n) L.vm[n][key] = (uint16_t)(wv[n] >> 16);
-          }
-        }
-        __syncthreads();
-        if (t + 1 < t1) issue(t + 1, page_for(t + 1));
+        PromptTile<D>& L = tiles_lds[(t - t0) & 1];
+        __syncthreads();  // this tile is whole, and the other one is no longer read
+        if (t + 1 < t1) stage(tiles_lds[(t - t0 + 1) & 1]);
+        if (t + 2 < t1) issue(t + 2);
 
-        // logits of keys 16 k + 4 g4 + j
+        // products with keys 16 k + 4 g4 + j
         f4 sc[2][4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
           const u4 km = *reinterpret_cast<const u4*>(&L.km[k * 16 + i16][0]);
-          sc[0][k] = mfma(km, sqb[0], f4{0.f, 0.f, 0.f, 0.f});
-          sc[1][k] = mfma(km, sqb[1], f4{0.f, 0.f, 0.f, 0.f});
+          sc[0][k] = mfma_f16(km, sqb[0], f4{0.f, 0.f, 0.f, 0.f});
+          sc[1][k] = mfma_f16(km, sqb[1], f4{0.f, 0.f, 0.f, 0.f});
 #pragma unroll
           for (int st = 0; st < KS; ++st) {
             const u4 ka = *reinterpret_cast<const u4*>(L.k + (k * 16 + i16) * kRow<D> + (st * 4 + g4) * 16);
+            sc[0][k] = mfma_f16(ka, qb[0][st], sc[0][k]);
+            sc[1][k] = mfma_f16(ka, qb[1][st], sc[1][k]);
+          }
+        }
+        if (scaled) {
+          asm volatile("");
 #pragma unroll
-            for (int p = 0; p < QP; ++p) {
-              sc[0][k] = mfma(ka, qb[0][p][st], sc[0][k]);
-              sc[1][k] = mfma(ka, qb[1][p][st], sc[1][k]);
-            }
+          for (int c = 0; c < 2; ++c)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) sc[c][k] *= qf[c];
+        }
+        // logits and the values' exponents
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const f4 kf = *reinterpret_cast<const f4*>(&L.kf[k * 16 + g4 * 4]);
+          const f4 ve = *reinterpret_cast<const f4*>(&L.ve[k * 16 + g4 * 4]);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            sc[0][k][j] = fmaf(sc[0][k][j], kf[j], ve[j]);
+            sc[1][k][j] = fmaf(sc[1][k][j], kf[j], ve[j]);
           }
         }
         const int r0 = t * KT;
-        const bool mask = r0 + KT > lim_all;
-        u4 hi[2][2], lo[2][2];
+        if (r0 + KT > lim_all) {
+          asm volatile("");
 #pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          if (mask) {
+          for (int c = 0; c < 2; ++c)
 #pragma unroll
             for (int k = 0; k < 4; ++k)
 #pragma unroll
               for (int j = 0; j < 4; ++j)
                 if (r0 + k * 16 + g4 * 4 + j >= lim[c]) sc[c][k][j] = -INFINITY;
-          }
+        }
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
           float mx = -INFINITY;
 #pragma unroll
           for (int k = 0; k < 4; ++k)
 #pragma unroll
             for (int j = 0; j < 4; ++j) mx = fmaxf(mx, sc[c][k][j]);
-          mx *= a.scale_log2;
           if (__builtin_amdgcn_ballot_w64(mx > m[c] + kLazy)) {
             mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
             mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
@@ -868,39 +947,38 @@ __global__ __launch_bounds__(256, 2) void page_prompt_kernel(PageAttendArgs a, i
 #pragma unroll
             for (int d = 0; d < DT; ++d) acc[c][d] *= alpha;
           }
+        }
+        u4 p[2][2];
 #pragma unroll
-          for (int half = 0; half < 2; ++half) {
-            float e[8];
+        for (int k = 0; k < 4; ++k) {
+          const f4 vi = *reinterpret_cast<const f4*>(&L.vi[k * 16 + g4 * 4]);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              e[i] = __builtin_amdgcn_exp2f(fmaf(sc[c][2 * half + (i >> 2)][i & 3], a.scale_log2, -m[c]));
-              l[c] += e[i];
+          for (int c = 0; c < 2; ++c) {
+            float e[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              e[j] = __builtin_amdgcn_exp2f(sc[c][k][j] - m[c]);
+              l[c] = fmaf(e[j], vi[j], l[c]);
             }
-            split_p(e, hi[c][half], lo[c][half]);
+            p[c][k >> 1][2 * (k & 1)] = h2(e[0], e[1]);
+            p[c][k >> 1][2 * (k & 1) + 1] = h2(e[2], e[3]);
           }
         }
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
-          const uint16_t* vm = &L.vm[i16 & (NG - 1)][half * 32 + g4 * 4];
+          const _Float16* vm = &L.vm[i16 & (NG - 1)][half * 32 + g4 * 4];
           const uint2 v0 = *reinterpret_cast<const uint2*>(vm), v1 = *reinterpret_cast<const uint2*>(vm + 16);
           const u4 va{v0.x, v0.y, v1.x, v1.y};
-#pragma unroll
-          for (int c = 0; c < 2; ++c) {
-            low[c] = mfma(va, hi[c][half], low[c]);
-            low[c] = mfma(va, lo[c][half], low[c]);
-          }
+          low[0] = mfma_f16(va, p[0][half], low[0]);
+          low[1] = mfma_f16(va, p[1][half], low[1]);
           const char* vb = (const char*)L.v + (half * 32 + g4 * 4 + (i16 >> 2)) * kRow<D> + (i16 & 3) * 8;
 #pragma unroll
           for (int d = 0; d < DT; ++d) {
             const u4 vt = ds_tr(vb + d * 32, vb + 16 * kRow<D> + d * 32);
-#pragma unroll
-            for (int c = 0; c < 2; ++c) {
-              acc[c][d] = mfma(vt, hi[c][half], acc[c][d]);
-              acc[c][d] = mfma(vt, lo[c][half], acc[c][d]);
-            }
+            acc[0][d] = mfma_f16(vt, p[0][half], acc[0][d]);
+            acc[1][d] = mfma_f16(vt, p[1][half], acc[1][d]);
           }
         }
-        __syncthreads();  // the tile's LDS is written again
       }
     }
 
@@ -914,27 +992,28 @@ __global__ __launch_bounds__(256, 2) void page_prompt_kernel(PageAttendArgs a, i
       ls += __shfl_xor(ls, 32, 64);
       if (any_bad) ls = __builtin_nanf("");
       const int r = wave * 32 + c * 16 + i16;
-      if (r >= rows) continue;
-      if (begins && ends) {
-        const float inv = ls == 0.0f ? 0.0f : 1.0f / ls;
+      const float inv = begins && ends ? (ls == 0.0f ? 0.0f : 1.0f / ls) : 1.0f;
+      const bool odd = g4 & 1;
 #pragma unroll
-        for (int d = 0; d < DT; ++d) {
-          f4 y = acc[c][d];
+      for (int d = 0; d < DT; ++d) {
+        f4 y = acc[c][d];
 #pragma unroll
-          for (int j = 0; j < 4; ++j) y[j] = (y[j] + low[c][d * NG / DT]) * inv;
-          const uint2 z = QP == 1 ? uint2{bf2(y[0], y[1]), bf2(y[2], y[3])} : uint2{h2(y[0], y[1]), h2(y[2], y[3])};
-          *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.o) + tok[c] * D + d * 16 + g4 * 4) = z;
+        for (int j = 0; j < 4; ++j) y[j] = (y[j] + low[c][d * NG / DT]) * inv;
+        // channels 0 4 1 5 and 2 6 3 7 of eight -> 0 .. 3 and 4 .. 7
+        const float r0 = __shfl_xor(odd ? y[0] : y[1], 16, 64), r1 = __shfl_xor(odd ? y[2] : y[3], 16, 64);
+        const f4 z = odd ? f4{r0, r1, y[1], y[3]} : f4{y[0], y[2], r0, r1};
+        if (r >= rows) continue;
+        if (begins && ends) {
+          const uint2 v = q_f16 ? uint2{h2(z[0], z[1]), h2(z[2], z[3])} : uint2{bf2(z[0], z[1]), bf2(z[2], z[3])};
+          *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.o) + tok[c] * D + d * 16 + g4 * 4) = v;
+        } else {
+          *reinterpret_cast<f4*>(out + r * kRec<D> + d * 16 + g4 * 4) = z;
         }
-        if (g4 == 0 && a.lse) a.lse[tok[c]] = lse_of(m[c], ls);
-      } else {
-#pragma unroll
-        for (int d = 0; d < DT; ++d) {
-          f4 y = acc[c][d];
-#pragma unroll
-          for (int j = 0; j < 4; ++j) y[j] += low[c][d * NG / DT];
-          *reinterpret_cast<f4*>(out + r * kRec<D> + d * 16 + g4 * 4) = y;
-        }
-        if (g4 == 0) {
+      }
+      if (g4 == 0 && r < rows) {
+        if (begins && ends) {
+          if (a.lse) a.lse[tok[c]] = lse_of(m[c], ls);
+        } else {
           out[r * kRec<D> + D] = m[c];
           out[r * kRec<D> + D + 1] = ls;
         }
@@ -949,7 +1028,7 @@ __global__ __launch_bounds__(256, 2) void page_prompt_kernel(PageAttendArgs a, i
       do {
         if (++s >= a.S) return;
         x = seq_of(a, s);
-        nb = prompt_blocks(x, G);
+        nb = prompt_blocks<WV>(x, G);
       } while (nb == 0);
     }
   }
@@ -1022,9 +1101,15 @@ static size_t records_at(const PageCache& pc, int S) {
   return align_up((size_t)pieces(pc) * pc.Hkv * sizeof(Cut)) + align_up(((size_t)S + 1) * sizeof(int));
 }
 
+// eight waves a workgroup where blocks of 256 rows are well filled
+static bool wide_prompt(int max_q, int G) { return (int64_t)max_q * G >= 512; }
+
 size_t page_attend_workspace(const PageCache& pc, int G, int S, int max_q) {
-  const size_t W = pieces(pc), rows = (int64_t)max_q * G > 16 ? QROWS : 16;
-  return records_at(pc, S) + (W > 1 ? W * pc.Hkv * 2 * rows * (pc.D + 4) * sizeof(float) : 0);
+  const size_t W = pieces(pc);
+  if (W == 1) return records_at(pc, S);
+  // (prompts: half the workgroups where they have twice the rows)
+  const size_t rows = (int64_t)max_q * G <= 16 ? 16 : kQRows<4>;
+  return records_at(pc, S) + W * pc.Hkv * 2 * rows * (pc.D + 4) * sizeof(float);
 }
 
 template <int D, int NG, int QP>
@@ -1039,10 +1124,16 @@ static void launch_matrix(const PageAttendArgs& a, int max_q, void* ws, hipStrea
   hipLaunchKernelGGL((page_tokens_kernel<D, NG, QP>), dim3(n), dim3(256), 0, st, a, Wt, rec, cuts);
   if (Wt > 1) hipLaunchKernelGGL((page_merge_kernel<D, 16, QT>), dim3(n, 2), dim3(256), 0, st, a, rec, cuts);
   if ((int64_t)max_q * a.G <= 16) return;
-  const int np = W * a.pc.Hkv;
-  hipLaunchKernelGGL(page_plan_kernel, dim3(1), dim3(1024), 0, st, a, units);
-  hipLaunchKernelGGL((page_prompt_kernel<D, NG, QP>), dim3(np), dim3(256), 0, st, a, W, units, rec, cuts);
-  if (W > 1) hipLaunchKernelGGL((page_merge_kernel<D, QROWS, QT>), dim3(np, 16), dim3(256), 0, st, a, rec, cuts);
+  auto prompts = [&](auto waves) {
+    constexpr int WV = decltype(waves)::value;
+    const int Wp = W * 4 / WV > 1 ? W * 4 / WV : 1, np = Wp * a.pc.Hkv;  // workgroups of WV waves: two waves per SIMD
+    hipLaunchKernelGGL(page_plan_kernel<WV>, dim3(1), dim3(1024), 0, st, a, units);
+    hipLaunchKernelGGL((page_prompt_kernel<D, NG, WV>), dim3(np), dim3(64 * WV), 0, st, a, Wp, QP == 2, units, rec, cuts);
+    if (Wp > 1)
+      hipLaunchKernelGGL((page_merge_kernel<D, kQRows<WV>, QT>), dim3(np, 16), dim3(256), 0, st, a, rec, cuts);
+  };
+  if (wide_prompt(max_q, a.G)) prompts(std::integral_constant<int, 8>{});
+  else prompts(std::integral_constant<int, 4>{});
 }
 
 hipError_t launch_page_valu(const PageAttendArgs& a, int q_dt, hipStream_t st) {
