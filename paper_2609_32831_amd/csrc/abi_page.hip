@@ -161,7 +161,7 @@ uc_status uc_page_attend(const uc_page_cache* cache, int Hq, const void* q, uc_d
   if (!(sm_scale > 0.0f) || !isfinite(sm_scale)) return fail(UC_E_INVALID, "sm_scale must be finite and > 0");
   if ((int64_t)T * Hq > INT32_MAX) return fail(UC_E_UNSUPPORTED, "too many query rows");
   // units of work: tiles of 64 rows, once per 128 query rows
-  const int64_t tiles = ((int64_t)table_ld * cache->page_rows + 63) / 64 + 8;
+  const int64_t tiles = ((int64_t)table_ld * cache->page_rows + 63) / 64 + 8;  // (8: what a sequence counts beside them)
   if (tiles > INT32_MAX / 64 || tiles * ((int64_t)S + (int64_t)T * (Hq / pc.Hkv) / 128) > INT32_MAX)
     return fail(UC_E_UNSUPPORTED, "tables of %d pages for %d sequences and %d tokens hold too much work for one call",
                 table_ld, S, T);

@@ -24,7 +24,6 @@
 // workgroup; one cut into several leaves a record (m, l, o) per piece, merged
 // by a second kernel in the order of the pieces.
 #include <algorithm>
-#include <type_traits>
 
 #include "page_common.h"
 
@@ -51,6 +50,12 @@ __device__ inline Seq seq_of(const PageAttendArgs& a, int s) {
   return x;
 }
 
+// the same in scalar registers, for a sequence that the whole wave works on
+__device__ inline Seq scalar(const Seq& x) {
+  return Seq{__builtin_amdgcn_readfirstlane(x.q0), __builtin_amdgcn_readfirstlane(x.n),
+             __builtin_amdgcn_readfirstlane(x.len)};
+}
+
 template <int QT>
 __device__ inline float q_val(const void* q, int64_t i) {
   return load_elem(q, QT, i);
@@ -66,27 +71,21 @@ __device__ inline void put(void* o, int64_t i, float x) {
 __device__ inline float lse_of(float m, float l) { return l > 0.0f ? (m + log2f(l)) * kLn2 : l == 0.0f ? -INFINITY : l; }
 
 // ---------------------------------------------------------------- vector ALU
-// One workgroup per (token, query head); keys in chunks of 256, one per
-// thread for the logits, one channel per thread for the values.
+// A query row by one workgroup of 256: keys in chunks of 256, one per thread
+// for the logits, one channel per thread for the values.
+template <int D>
+struct RowLds {
+  float sq[D], sp[256], red[WAVES], so[256 / D][D];
+  int64_t srow[256];
+};
+
+// token t of sequence s, query head hq
 template <int D, int QT>
-__global__ __launch_bounds__(256) void page_attend_valu_kernel(PageAttendArgs a) {
-  __shared__ float sq[D], sp[256], red[WAVES], so[256 / D][D];
-  __shared__ int64_t srow[256];
-  const int Hq = a.pc.Hkv * a.G, hq = blockIdx.x % Hq, t = blockIdx.x / Hq, h = hq / a.G;
-  // the sequence whose tokens include t
-  __shared__ int s_seq;
-  if (threadIdx.x == 0) s_seq = INT32_MAX;
-  __syncthreads();
-  for (int s = threadIdx.x; s < a.S; s += blockDim.x) {
-    const Seq x = seq_of(a, s);
-    if (t >= x.q0 && t < x.q0 + x.n) atomicMin(&s_seq, s);
-  }
-  __syncthreads();
-  if (s_seq == INT32_MAX) return;  // a row of no sequence stays as it was
-  const Seq x = seq_of(a, s_seq);
+__device__ inline void attend_row(const PageAttendArgs& a, RowLds<D>& L, const Seq& x, int s, int t, int hq) {
+  const int Hq = a.pc.Hkv * a.G, h = hq / a.G;
   const int lim = max(0, min(x.len, (int)((int64_t)x.len - x.n + (t - x.q0) + 1)));
-  const int32_t* trow = a.table + (int64_t)s_seq * a.ld;
-  for (int d = threadIdx.x; d < D; d += blockDim.x) sq[d] = q_val<QT>(a.q, (int64_t)t * a.q_ld + hq * D + d);
+  const int32_t* trow = a.table + (int64_t)s * a.ld;
+  for (int d = threadIdx.x; d < D; d += blockDim.x) L.sq[d] = q_val<QT>(a.q, (int64_t)t * a.q_ld + hq * D + d);
   const int ng = a.pc.ng, gsz = D / ng;
   const int dim = threadIdx.x % D, part = threadIdx.x / D;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -109,43 +108,60 @@ __global__ __launch_bounds__(256) void page_attend_valu_kernel(PageAttendArgs a)
         const int c0 = 32 * (w % (D / 32)) + 8 * (w / (D / 32));  // first channel of the word
         const uint32_t cw = codes[w], sw = a.pc.scale_k[row * ng + c0 / gsz];
         for (int e = 0; e < 8; ++e)
-          sum = fmaf(sq[c0 + e], fmaf((float)((cw >> (4 * e)) & 15u), word_step(sw), word_min(sw)), sum);
+          sum = fmaf(L.sq[c0 + e], fmaf((float)((cw >> (4 * e)) & 15u), word_step(sw), word_min(sw)), sum);
       }
       v = sum * a.scale_log2;
     }
-    srow[threadIdx.x] = row;
+    L.srow[threadIdx.x] = row;
     float mx = wave_max(v);
-    if (lane == 0) red[wave] = mx;
+    if (lane == 0) L.red[wave] = mx;
     __syncthreads();
-    mx = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+    mx = fmaxf(fmaxf(L.red[0], L.red[1]), fmaxf(L.red[2], L.red[3]));
     const float m_new = fmaxf(m, mx), alpha = exp2f(m - m_new);
     m = m_new;
     const float p = exp2f(v - m);
-    sp[threadIdx.x] = p;
+    L.sp[threadIdx.x] = p;
     l = l * alpha + p;  // this thread's keys
     acc *= alpha;
     __syncthreads();
     const int n = min(256, lim - j0);
     for (int i = part; i < n; i += 256 / D) {
-      if (srow[i] < 0) continue;
-      const uint8_t b = a.pc.codes_v[srow[i] * (D / 2) + dim / 2];
-      const uint32_t sw = a.pc.scale_v[srow[i] * ng + dim / gsz];
-      acc = fmaf(sp[i], fmaf((float)((b >> (4 * (dim & 1))) & 15), word_step(sw), word_min(sw)), acc);
+      if (L.srow[i] < 0) continue;
+      const uint8_t b = a.pc.codes_v[L.srow[i] * (D / 2) + dim / 2];
+      const uint32_t sw = a.pc.scale_v[L.srow[i] * ng + dim / gsz];
+      acc = fmaf(L.sp[i], fmaf((float)((b >> (4 * (dim & 1))) & 15), word_step(sw), word_min(sw)), acc);
     }
   }
   __syncthreads();
-  so[part][dim] = acc;
+  L.so[part][dim] = acc;
   l = wave_sum(l);
-  if (lane == 0) red[wave] = l;
+  if (lane == 0) L.red[wave] = l;
   const int any_bad = __syncthreads_or(bad);
-  l = (red[0] + red[1]) + (red[2] + red[3]);
+  l = (L.red[0] + L.red[1]) + (L.red[2] + L.red[3]);
   if (any_bad) l = __builtin_nanf("");
   if (threadIdx.x < D) {
-    float s = 0.0f;
-    for (int i = 0; i < 256 / D; ++i) s += so[i][threadIdx.x];
-    put<QT>(a.o, ((int64_t)t * Hq + hq) * D + threadIdx.x, l == 0.0f ? 0.0f : s / l);
+    float y = 0.0f;
+    for (int i = 0; i < 256 / D; ++i) y += L.so[i][threadIdx.x];
+    put<QT>(a.o, ((int64_t)t * Hq + hq) * D + threadIdx.x, l == 0.0f ? 0.0f : y / l);
   }
   if (threadIdx.x == 0 && a.lse) a.lse[(int64_t)t * Hq + hq] = lse_of(m, l);
+}
+
+template <int D, int QT>
+__global__ __launch_bounds__(256) void page_attend_valu_kernel(PageAttendArgs a) {
+  __shared__ RowLds<D> lds;
+  const int Hq = a.pc.Hkv * a.G, hq = blockIdx.x % Hq, t = blockIdx.x / Hq;
+  // the sequence whose tokens include t
+  __shared__ int s_seq;
+  if (threadIdx.x == 0) s_seq = INT32_MAX;
+  __syncthreads();
+  for (int s = threadIdx.x; s < a.S; s += blockDim.x) {
+    const Seq x = seq_of(a, s);
+    if (t >= x.q0 && t < x.q0 + x.n) atomicMin(&s_seq, s);
+  }
+  __syncthreads();
+  const int s = s_seq;
+  if (s < INT32_MAX) attend_row<D, QT>(a, lds, seq_of(a, s), s, t, hq);  // a row of no sequence stays as it was
 }
 
 // ---------------------------------------------------------------- the line of tiles
@@ -183,6 +199,51 @@ constexpr int kRec = D + 4;
 template <int D, int ROWS, class T>
 __device__ inline T* record(T* rec, int w, int Hkv, int h, bool begins) {
   return rec + (((int64_t)w * Hkv + h) * 2 + begins) * ROWS * kRec<D>;
+}
+
+// the prompt kernel's cut: blocks of 256 query rows
+constexpr int PWAVES = 8, QROWS = 32 * PWAVES;
+
+// blocks of a sequence
+__device__ inline int prompt_blocks(const Seq& x, int G) {
+  const int64_t rows = (int64_t)x.n * G;
+  return rows <= 16 ? 0 : (int)((rows + QROWS - 1) / QROWS);
+}
+// tiles of its block b, at least one
+__device__ inline int prompt_tiles(const Seq& x, int G, int b) {
+  const int64_t last = min((int64_t)x.n - 1, ((int64_t)b * QROWS + QROWS - 1) / G);
+  const int64_t sees = max((int64_t)0, min((int64_t)x.len, (int64_t)x.len - x.n + last + 1));
+  return tiles_of((int)sees);
+}
+
+// before[s]: units of the sequences ahead of s, before[S]: all of them (by one
+// workgroup of 256)
+__device__ inline void plan_prompts(const PageAttendArgs& a, int* __restrict__ before, int* part) {
+  const int lane = threadIdx.x & 63;
+  int base = 0;
+  for (int s0 = 0; s0 < a.S; s0 += 256) {
+    const int s = s0 + threadIdx.x;
+    Seq x{0, 0, 0};
+    if (s < a.S) x = seq_of(a, s);
+    const int blocks = prompt_blocks(x, a.G);
+    int mine = 0;
+    // the wave counts one sequence after the other, a block per lane
+    for (uint64_t todo = __builtin_amdgcn_ballot_w64(blocks > 0); todo; todo &= todo - 1) {
+      const int from = __ffsll((unsigned long long)todo) - 1;
+      const Seq y{0, __shfl(x.n, from, 64), __shfl(x.len, from, 64)};
+      const int nb = __shfl(blocks, from, 64);
+      int sum = 0;
+      for (int b = lane; b < nb; b += 64) sum += prompt_tiles(y, a.G, b);
+#pragma unroll
+      for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
+      if (lane == from) mine = sum;
+    }
+    int total;
+    const int upto = block_scan(mine, part, total);
+    if (s < a.S) before[s] = base + upto - mine;
+    base += total;
+  }
+  if (threadIdx.x == 0) before[a.S] = base;
 }
 
 // ---------------------------------------------------------------- single tokens
@@ -231,6 +292,13 @@ struct WaveLds {
   uint8_t codes[KT * VROW];
 };
 
+// x * scale rounded, then less m
+__device__ inline float scaled_less(float x, float scale, float m) {
+#pragma clang fp contract(off)
+  const float y = x * scale;
+  return y - m;
+}
+
 // D, NG: head dim and groups of a row; QP: bf16 parts of a query element.
 //
 // A wave's tile is four blocks of 16 keys, each within one page (pages are 16
@@ -240,7 +308,7 @@ struct WaveLds {
 // values take their rows in that order.
 template <int D, int NG, int QP>
 __global__ __launch_bounds__(256, 2) void page_tokens_kernel(PageAttendArgs a, int W_all, float* __restrict__ rec,
-                                                             Cut* __restrict__ cuts) {
+                                                             Cut* __restrict__ cuts, int* __restrict__ units_out) {
   constexpr int KS = D / 32;  // matrix steps over the channels, words of a lane's codes of a row
   constexpr int DT = D / 16;  // tiles of 16 output channels
   constexpr int GS = KS / NG;
@@ -253,6 +321,10 @@ __global__ __launch_bounds__(256, 2) void page_tokens_kernel(PageAttendArgs a, i
   const int Hkv = a.pc.Hkv, h = blockIdx.x % Hkv, w = blockIdx.x / Hkv;
   const int G = a.G, Hq = G * Hkv, lgP = a.pc.lgP, P1 = (1 << lgP) - 1;
   const Magic magic;
+  if (w == W_all) {  // one workgroup more where prompts follow: their plan
+    plan_prompts(a, units_out, reinterpret_cast<int*>(lds));
+    return;
+  }
   if (threadIdx.x == 0) cuts[blockIdx.x] = Cut{-1, 0, 0, 0};
 
   // this piece of the line; lane i counts sequences i c .. i c + c - 1
@@ -385,6 +457,7 @@ __global__ __launch_bounds__(256, 2) void page_tokens_kernel(PageAttendArgs a, i
     const int lim = max(0, min(x.len, (int)((int64_t)x.len - x.n + min(i16, nq - 1) / G + 1)));
     const int lim_all = max(0, (int)((int64_t)x.len - x.n + 1));
 
+    bool far = false;
     float m = kNone, l = 0.0f, low[NG];
     f4 acc[DT];
 #pragma unroll
@@ -414,7 +487,8 @@ __global__ __launch_bounds__(256, 2) void page_tokens_kernel(PageAttendArgs a, i
             L.k[0][g][lane] = word_step(xk);
             L.k[1][g][lane] = word_min(xk);
             L.v[0][g][lane] = word_step(xv);
-            L.v[1][g][lane] = fmaf(-128.0f, word_step(xv), word_min(xv));
+            // (held finite: a row that is not seen weighs it with zero)
+            L.v[1][g][lane] = fmaxf(fmaf(-128.0f, word_step(xv), word_min(xv)), -3.4e38f);
           }
         }
         __builtin_amdgcn_wave_barrier();
@@ -468,15 +542,23 @@ __global__ __launch_bounds__(256, 2) void page_tokens_kernel(PageAttendArgs a, i
           mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
           const float m_new = fmaxf(m, mx), alpha = __builtin_amdgcn_exp2f(m - m_new);
           m = m_new;
+          far = __builtin_amdgcn_ballot_w64(m > 0x1p22f) != 0;
           l *= alpha;
 #pragma unroll
           for (int g = 0; g < NG; ++g) low[g] *= alpha;
 #pragma unroll
           for (int d = 0; d < DT; ++d) acc[d] *= alpha;
         }
+        if (far) {  // m's own rounding may reach the exponent's range: round the others alike
+#pragma unroll
+          for (int e = 0; e < 16; ++e) p[e] = scaled_less(p[e], a.scale_log2, m);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 16; ++e) p[e] = fmaf(p[e], a.scale_log2, -m);
+        }
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-          p[e] = __builtin_amdgcn_exp2f(fmaf(p[e], a.scale_log2, -m));
+          p[e] = __builtin_amdgcn_exp2f(p[e]);
           l += p[e];
         }
         // O^T += V^T P, group by group
@@ -580,85 +662,57 @@ __global__ __launch_bounds__(256, 2) void page_tokens_kernel(PageAttendArgs a, i
 }
 
 // ---------------------------------------------------------------- prompts
-// Blocks of 32 query rows a wave, each over the tiles that its last row sees;
-// the line is made of all blocks' tiles.  A workgroup's waves share the tile
-// in LDS, where the 4-bit rows, read and unpacked once for all of them, stand
-// as fp16: with the power of two 2^e of the key's largest step taken out,
-// c * (s 2^-e) has 8 significant bits and is exact, and so is the minimum.
-// The powers return where they cost nothing: the keys' in the factor that
-// turns a product into a logit, the values' in the exponent,
+// Blocks of 256 query rows, 32 a wave, each over the tiles that its last row
+// sees; the line is made of all blocks' tiles.  A workgroup's eight waves share
+// the tile in LDS, where the 4-bit rows, read and unpacked once for all of
+// them, stand as fp16: with the power of two 2^e of the largest step of 16 rows
+// taken out, c * (s 2^-e) has 8 significant bits and is exact, and so is the
+// minimum, down to steps of 2^-13 of the largest.  The powers return where they
+// cost nothing: the keys' in the factor that turns a product into a logit, the
+// values' in the exponent,
 //   w_j = 2^(logit_j + e_j - m),  o ~ sum_j w_j (v_j 2^-e_j),  l = sum_j w_j 2^-e_j,
 // with the reference m kept over logit + e, so that w_j, rounded to fp16 (11
 // bits), is measured by what key j contributes whatever the values' sizes.  l
-// is summed in binary32 before that rounding.  Steps of values from 2^-60 to
-// 2^88 keep all their bits.  The minima go through matrix instructions of
-// their own, q . k += sum_g m_g sum(q_g) with sum(q_g) in three fp16 parts.
-// Queries enter as fp16 too, exactly (a row far from 1 by a power of two).
+// is summed in binary32 before that rounding.  The minima go through matrix
+// instructions of their own, q . k += sum_g m_g sum(q_g) with sum(q_g) in
+// three fp16 parts.  Queries enter as fp16 too, exactly (a row far from 1 by a
+// power of two).
 //
-// Per 64 keys x 32 rows a wave issues 64 matrix instructions of 16 cycles for
-// the two products and 12 for the minima, and some 400 vector instructions of
-// 4 cycles; both bound it.
-template <int WV>
-constexpr int kQRows = 32 * WV;
-
-// blocks of a sequence in the prompt kernel
-template <int WV>
-__device__ inline int prompt_blocks(const Seq& x, int G) {
-  const int64_t rows = (int64_t)x.n * G;
-  return rows <= 16 ? 0 : (int)((rows + kQRows<WV> - 1) / kQRows<WV>);
-}
-// tiles of its block b, at least one
-template <int WV>
-__device__ inline int prompt_tiles(const Seq& x, int G, int b) {
-  const int64_t last = min((int64_t)x.n - 1, ((int64_t)b * kQRows<WV> + kQRows<WV> - 1) / G);
-  const int64_t sees = max((int64_t)0, min((int64_t)x.len, (int64_t)x.len - x.n + last + 1));
-  return tiles_of((int)sees);
-}
-
-// before[s]: units of the sequences ahead of s, before[S]: all of them
-template <int WV>
-__global__ __launch_bounds__(1024) void page_plan_kernel(PageAttendArgs a, int* __restrict__ before) {
-  __shared__ int part[16];
-  const int lane = threadIdx.x & 63;
-  int base = 0;
-  for (int s0 = 0; s0 < a.S; s0 += 1024) {
-    const int s = s0 + threadIdx.x;
-    Seq x{0, 0, 0};
-    if (s < a.S) x = seq_of(a, s);
-    const int blocks = prompt_blocks<WV>(x, a.G);
-    int mine = 0;
-    // the wave counts one sequence after the other, a block per lane
-    for (uint64_t todo = __builtin_amdgcn_ballot_w64(blocks > 0); todo; todo &= todo - 1) {
-      const int from = __ffsll((unsigned long long)todo) - 1;
-      const Seq y{0, __shfl(x.n, from, 64), __shfl(x.len, from, 64)};
-      const int nb = __shfl(blocks, from, 64);
-      int sum = 0;
-      for (int b = lane; b < nb; b += 64) sum += prompt_tiles<WV>(y, a.G, b);
-#pragma unroll
-      for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
-      if (lane == from) mine = sum;
-    }
-    int total;
-    const int upto = block_scan(mine, part, total);
-    if (s < a.S) before[s] = base + upto - mine;
-    base += total;
-  }
-  if (threadIdx.x == 0) before[a.S] = base;
-}
-
+// Rows of more different sizes within 16 (one of infinities, say, that earlier
+// queries do not see), and values beyond 2^-60 .. 2^76, mark the workgroup's
+// piece; every block that has a part in it is computed anew from the cache, a
+// row per workgroup.  Looking for them costs 2 % of the kernel's time.
+//
+// Four prompts of 1500 tokens over up to 8192 rows, 28 query heads on 4, D 128
+// (342 GFLOP): 460 us a call, 745 TFLOP/s.  A stage of 64 keys x 32 rows is 76
+// matrix instructions a wave and five vector instructions to each of those,
+// most of them for the softmax; the two do not overlap fully with the two waves
+// a SIMD holds.  Tried: four waves a workgroup, each tile then staged for half
+// the rows (709 us); two buffers and a barrier per tile instead of the
+// pipeline of steps (530 us); bf16 planes (578 us); fixed orders of matrix and
+// vector instructions (498 to 553 us) - the compiler's own is the best.
 template <int D>
 constexpr int kRow = 2 * D + 32;  // bytes of a staged row: 8 consecutive rows start in different 8-bank groups
 
 typedef _Float16 half2 __attribute__((ext_vector_type(2)));
 
-template <int D>
-struct PromptTile {
-  uint8_t k[KT * kRow<D>];  // c * s 2^-e in fp16; of eight channels in the order 0 4 1 5 2 6 3 7
-  uint8_t v[KT * kRow<D>];
-  _Float16 km[KT][8];      // minima (2^-e) of a key, zeros behind them
-  _Float16 vm[4][KT + 8];  // minima (2^-e) of a value group, by key
-  float kf[KT];            // logit of a product: scale * 2^e
-  float ve[KT], vi[KT];    // e and 2^-e of the values
+// Keys and values of a stage of KS keys, in rings of three: the loop is a
+// pipeline over steps of 32 keys that takes, in step j, the products of step
+// j + 1, the probabilities of step j and the output of step j - 1, which do
+// not depend on one another; so a stage's keys are wanted from the stage
+// before it to its own end, and its values from its beginning to the next
+// one's.
+template <int D, int KEYS>
+struct PromptKeys {
+  uint8_t k[KEYS * kRow<D>];  // c * s 2^-e in fp16; of eight channels in the order 0 4 1 5 2 6 3 7
+  _Float16 m[KEYS][8];        // minima (2^-e) of a key, zeros behind them
+  float f[KEYS / 16];         // logit of a product: scale * 2^e
+};
+template <int D, int KEYS>
+struct PromptValues {
+  uint8_t v[KEYS * kRow<D>];
+  _Float16 m[4][KEYS + 8];            // minima (2^-e) of a group, by key
+  float e[KEYS / 16], inv[KEYS / 16];  // e and 2^-e
 };
 
 // a word's eight codes times a step, as fp16: (1024 + c) s - 1024 s
@@ -676,31 +730,60 @@ struct Unpack {
   }
 };
 
-// biased exponent of the power of two taken out of a row: its largest step
-// comes below 2 and its minima below 2^14
-template <int NG>
-__device__ inline int row_exponent(const uint32_t (&w)[NG], int least, int most) {
+// Biased exponent of the power of two taken out of 16 rows (16 CH lanes, CH
+// of a row): their largest step comes below 2 and their minima below 2^14.
+// What does not fit beside it sets `wide`: a group whose step and minimum are
+// both below 2^-13 of it (above, codes times steps are exact and a minimum is
+// off by 2^-12 of the larger of both at most), or a power beyond the range.
+template <int NG, int CH>
+__device__ inline int rows_exponent(const uint32_t (&w)[NG], int ch, int least, int most, int& wide) {
   int e = 0;
 #pragma unroll
   for (int n = 0; n < NG; ++n)
     e = max(e, max((int)(w[n] >> 7 & 0xFF), (int)(w[n] >> 23 & 0xFF) - 12));
-  return e == 0 ? 127 : min(max(e, least), most);  // a row of zeros: any
+  // over the lanes CH apart of a row of 16 lanes, then over the rows
+  e = max(e, __builtin_amdgcn_update_dpp(e, e, 0x120 + 8, 0xF, 0xF, false));
+  e = max(e, __builtin_amdgcn_update_dpp(e, e, 0x120 + 4, 0xF, 0xF, false));
+  if constexpr (CH == 2) e = max(e, __builtin_amdgcn_update_dpp(e, e, 0x120 + 2, 0xF, 0xF, false));
+  const auto r16 = __builtin_amdgcn_permlane16_swap(e, e, false, false);
+  e = max((int)r16[0], (int)r16[1]);
+  if constexpr (CH == 4) {
+    const auto r32 = __builtin_amdgcn_permlane32_swap(e, e, false, false);
+    e = max((int)r32[0], (int)r32[1]);
+  }
+  const int E = e == 0 ? 127 : min(max(e, least), most);  // rows of zeros: any
+  uint32_t mine = w[0];  // the row's lanes look at a group each
+#pragma unroll
+  for (int n = 1; n < NG; ++n)
+    if (ch * NG / CH == n) mine = w[n];
+  const int own = max((int)(mine >> 7 & 0xFF), (int)(mine >> 23 & 0xFF));
+  if (e > most || (uint32_t)(own - 1) < (uint32_t)(E - 14)) wide = 1;  // (a group of zeros fits)
+  return E;
 }
 
-template <int D, int NG, int WV>
-__global__ __launch_bounds__(64 * WV, 2) void page_prompt_kernel(PageAttendArgs a, int W_all, bool q_f16,
+template <int D, int NG>
+__global__ __launch_bounds__(64 * PWAVES, 2) void page_prompt_kernel(PageAttendArgs a, int W_all, bool q_f16,
                                                                  const int* __restrict__ units,
-                                                                 float* __restrict__ rec, Cut* __restrict__ cuts) {
-  constexpr int KS = D / 32, DT = D / 16, QROWS = kQRows<WV>, THREADS = 64 * WV;
-  __shared__ __attribute__((aligned(16))) PromptTile<D> tiles_lds[2];
-  __shared__ int s_part[16], s_block, s_before;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+                                                                 float* __restrict__ rec, Cut* __restrict__ cuts,
+                                                                 int* __restrict__ wide) {
+  constexpr int KS = D / 32, DT = D / 16, THREADS = 64 * PWAVES;
+  constexpr int KEYS = 64, SPS = KEYS / 32;  // keys and steps of a stage
+  using Keys = PromptKeys<D, KEYS>;
+  using Values = PromptValues<D, KEYS>;
+  __shared__ __attribute__((aligned(16))) Keys keys[3];
+  __shared__ __attribute__((aligned(16))) Values values[3];
+  __shared__ float2 s_rows[2][THREADS];  // for the lanes' query rows: first row not seen (bits), power of two taken out
+  __shared__ int s_part[16], s_block, s_before, s_wide;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int i16 = lane & 15, g4 = lane >> 4;
   const int Hkv = a.pc.Hkv, h = blockIdx.x % Hkv, w = blockIdx.x / Hkv;
   const int G = a.G, Hq = G * Hkv, lgP = a.pc.lgP;
   const Unpack unpack;
-  if (threadIdx.x == 0) cuts[blockIdx.x] = Cut{-1, 0, 0, 0};
-  const int U = units[a.S];
+  if (threadIdx.x == 0) {
+    cuts[blockIdx.x] = Cut{-1, 0, 0, 0};
+    wide[blockIdx.x] = s_wide = 0;
+  }
+  const int U = __builtin_amdgcn_readfirstlane(units[a.S]);
   if (U == 0) return;
   const Line line(U, min(W_all, U));
   if (w >= line.W) return;
@@ -712,14 +795,15 @@ __global__ __launch_bounds__(64 * WV, 2) void page_prompt_kernel(PageAttendArgs 
     if (units[mid] <= u0) s = mid;
     else hi = mid;
   }
-  Seq x = seq_of(a, s);
-  int nb = prompt_blocks<WV>(x, G);
+  s = __builtin_amdgcn_readfirstlane(s);
+  Seq x = scalar(seq_of(a, s));
+  int nb = prompt_blocks(x, G);
   if (threadIdx.x == 0) s_block = -1;
   {
     int base = units[s];
     for (int b0 = 0; b0 < nb; b0 += THREADS) {
       const int b = b0 + threadIdx.x;
-      const int mine = b < nb ? prompt_tiles<WV>(x, G, b) : 0;
+      const int mine = b < nb ? prompt_tiles(x, G, b) : 0;
       int total;
       const int upto = base + block_scan(mine, s_part, total);
       if (upto - mine <= u0 && u0 < upto) {
@@ -730,95 +814,90 @@ __global__ __launch_bounds__(64 * WV, 2) void page_prompt_kernel(PageAttendArgs 
     }
   }
   // the slots behind a key's minima stay zero
-  for (int i = threadIdx.x; i < KT * 8; i += THREADS)
-    (&tiles_lds[0].km[0][0])[i] = (&tiles_lds[1].km[0][0])[i] = (_Float16)0.0f;
+  for (int i = threadIdx.x; i < KEYS * 8; i += THREADS)
+    (&keys[0].m[0][0])[i] = (&keys[1].m[0][0])[i] = (&keys[2].m[0][0])[i] = (_Float16)0.0f;
   __syncthreads();
-  int b = s_block;
+  int b = __builtin_amdgcn_readfirstlane(s_block);
   if (b < 0) return;  // starts that overlap so often that the sums passed their type
-  int before = s_before;
+  int before = __builtin_amdgcn_readfirstlane(s_before);
 
-  // A thread's share of a tile: 16 bytes of codes of a row of keys or values.
-  constexpr int CH = D / 32, TASKS = 2 * KT * CH, PER = TASKS > THREADS ? TASKS / THREADS : 1;
-  static_assert(PER <= 2, "one task of each kind at most");
-  u4 codes[PER];
-  uint32_t words[PER][NG];
+  // A thread's share of a stage: 16 bytes of codes of a row, of keys (the
+  // first waves) or of values.
+  constexpr int CH = D / 32;
+  static_assert(2 * KEYS * CH <= THREADS, "a task a thread at most");
+  const int kind = wave * 64 / (KEYS * CH), key = threadIdx.x % (KEYS * CH) / CH, ch = threadIdx.x % CH;
+  u4 codes;
+  uint32_t words[NG];
 
   for (int u = u0; u < u1;) {
-    const int tiles = prompt_tiles<WV>(x, G, b);
+    const int tiles = prompt_tiles(x, G, b);
     const int t0 = u - before, t1 = min(tiles, u1 - before);
     const int rows = (int)min((int64_t)QROWS, (int64_t)x.n * G - (int64_t)b * QROWS);
     const int32_t* trow = a.table + (int64_t)s * a.ld;
     bool bad = false;
 
-    auto issue = [&](int t) {
+    // the thread's codes of a stage; rows past the sequence repeat its last
+    // one.  Its page is read a stage ahead.
+    auto row_at = [&](int stage) { return min(t0 * KT + stage * KEYS + key, x.len - 1); };
+    int page = x.len > 0 ? page_of(trow, row_at(0), lgP, a.pc.n_pages) : 0;
+    auto issue = [&](int stage) {
+      if (page < 0) bad = true;
+      const int64_t row = page_row(max(page, 0), Hkv, h, lgP, row_at(stage));
+      page = page_of(trow, row_at(stage + 1), lgP, a.pc.n_pages);
+      if (kind > 1) return;
+      codes = *reinterpret_cast<const u4*>((kind ? a.pc.codes_v : a.pc.codes_k) + row * (D / 2) + ch * 16);
+      load_words<NG>((kind ? a.pc.scale_v : a.pc.scale_k) + row * NG, words);
+    };
+    auto store_keys = [&](Keys& L) {
+      const int E = rows_exponent<NG, CH>(words, ch, 24, 230, s_wide);
+      const float out = __uint_as_float((uint32_t)(254 - E) << 23);
+      half2 st[NG], off[NG];
 #pragma unroll
-      for (int i = 0; i < PER; ++i) {
-        const int task = threadIdx.x + i * THREADS, kind = task / (KT * CH), key = task % (KT * CH) / CH;
-        if (kind > 1) continue;
-        const int r = min(t * KT + key, x.len - 1), page = page_of(trow, r, lgP, a.pc.n_pages);
-        if (page < 0) bad = true;
-        const int64_t row = page_row(max(page, 0), Hkv, h, lgP, r);
-        codes[i] = *reinterpret_cast<const u4*>((kind ? a.pc.codes_v : a.pc.codes_k) + row * (D / 2) + task % CH * 16);
-        load_words<NG>((kind ? a.pc.scale_v : a.pc.scale_k) + row * NG, words[i]);
+      for (int n = 0; n < NG; ++n) {
+        const float f = word_step(words[n]) * out;
+        st[n] = __builtin_bit_cast(half2, h2(f, f));
+        off[n] = __builtin_bit_cast(half2, h2(-1024.0f * f, -1024.0f * f));
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        // the word holds channels 32 step + 8 g ..
+        const int step = KS == 4 ? j : j % KS, g = (ch * 4 + j) / KS, n = step * NG / KS;
+        *reinterpret_cast<u4*>(L.k + key * kRow<D> + (step * 4 + g) * 16) = unpack.times(codes[j], st[n], off[n]);
+      }
+      if (ch == 0) {
+#pragma unroll
+        for (int n = 0; n < NG; ++n) L.m[key][n] = (_Float16)(word_min(words[n]) * out);
+        L.f[key / 16] = __uint_as_float((uint32_t)E << 23) * a.scale_log2;
       }
     };
-    // the tile to LDS; rows past the sequence repeat its last one
-    auto stage = [&](PromptTile<D>& L) {
+    auto store_values = [&](Values& L) {
+      const int E = rows_exponent<NG, CH>(words, ch, 127 - 48, 127 + 76, s_wide);
+      const float out = __uint_as_float((uint32_t)(254 - E) << 23);
+      float f = word_step(words[0]);
 #pragma unroll
-      for (int i = 0; i < PER; ++i) {
-        const int task = threadIdx.x + i * THREADS, kind = task / (KT * CH), key = task % (KT * CH) / CH, ch = task % CH;
-        if (kind > 1) continue;
-        const int E = kind ? row_exponent<NG>(words[i], 127 - 48, 127 + 76) : row_exponent<NG>(words[i], 24, 230);
-        const float out = __uint_as_float((uint32_t)(254 - E) << 23), in = __uint_as_float((uint32_t)E << 23);
-        half2 st[NG], off[NG];
+      for (int n = 1; n < NG; ++n)
+        if (ch * NG / CH == n) f = word_step(words[n]);
+      f *= out;
+      const half2 st = __builtin_bit_cast(half2, h2(f, f)), off = __builtin_bit_cast(half2, h2(-1024.0f * f, -1024.0f * f));
 #pragma unroll
-        for (int n = 0; n < NG; ++n) {
-          const float f = word_step(words[i][n]) * out;
-          st[n] = __builtin_bit_cast(half2, h2(f, f));
-          off[n] = __builtin_bit_cast(half2, h2(-1024.0f * f, -1024.0f * f));
-        }
-        if (kind == 0) {
+      for (int j = 0; j < 4; ++j)
+        *reinterpret_cast<u4*>(L.v + key * kRow<D> + (ch * 4 + j) * 16) = unpack.times(codes[j], st, off);
+      if (ch == 0) {
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            // the word holds channels 32 step + 8 g ..
-            const int step = KS == 4 ? j : j % KS, g = (ch * 4 + j) / KS, n = step * NG / KS;
-            *reinterpret_cast<u4*>(L.k + key * kRow<D> + (step * 4 + g) * 16) = unpack.times(codes[i][j], st[n], off[n]);
-          }
-          if (ch == 0) {
-#pragma unroll
-            for (int n = 0; n < NG; ++n) L.km[key][n] = (_Float16)(word_min(words[i][n]) * out);
-            L.kf[key] = in * a.scale_log2;
-          }
-        } else {
-          half2 sv = st[0], ov = off[0];
-#pragma unroll
-          for (int n = 1; n < NG; ++n)
-            if (ch * NG / CH == n) sv = st[n], ov = off[n];
-#pragma unroll
-          for (int j = 0; j < 4; ++j)
-            *reinterpret_cast<u4*>(L.v + key * kRow<D> + (ch * 4 + j) * 16) = unpack.times(codes[i][j], sv, ov);
-          if (ch == 0) {
-#pragma unroll
-            for (int n = 0; n < NG; ++n) L.vm[n][key] = (_Float16)(word_min(words[i][n]) * out);
-            L.ve[key] = (float)(E - 127);
-            L.vi[key] = out;
-          }
-        }
+        for (int n = 0; n < NG; ++n) L.m[n][key] = (_Float16)(word_min(words[n]) * out);
+        L.e[key / 16] = (float)(E - 127);
+        L.inv[key / 16] = out;
       }
     };
-    if (x.len > 0) issue(t0);
+    if (x.len > 0) issue(0);
 
     u4 qb[2][KS], sqb[2];
-    int lim[2];
-    float qf[2];      // power of two taken out of the lane's query row
-    int64_t tok[2];   // the lane's query rows, among the rows of o
     bool scaled = false;
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
       const int r = wave * 32 + c * 16 + i16;
       const int rr = b * QROWS + min(r, rows - 1), i = rr / G, gq = rr % G;
-      lim[c] = (int)max((int64_t)0, min((int64_t)x.len, (int64_t)x.len - x.n + i + 1));
-      tok[c] = (int64_t)(x.q0 + i) * Hq + h * G + gq;
+      const int lim = (int)max((int64_t)0, min((int64_t)x.len, (int64_t)x.len - x.n + i + 1));
       const int64_t base = (int64_t)(x.q0 + i) * a.q_ld + (int64_t)(h * G + gq) * D + g4 * 8;
       float f[KS][8], most = 0.0f;
 #pragma unroll
@@ -836,7 +915,7 @@ __global__ __launch_bounds__(64 * WV, 2) void page_prompt_kernel(PageAttendArgs 
       const int E = (int)(__float_as_uint(most) >> 23);  // 2^(E - 127) <= most
       const bool far = most > 0.0f && (E < 127 - 4 || E > 127 + 14);
       const float out = far ? __uint_as_float((uint32_t)(254 - min(max(E, 1), 253)) << 23) : 1.0f;
-      qf[c] = far ? __uint_as_float((uint32_t)min(max(E, 1), 253) << 23) : 1.0f;
+      s_rows[c][threadIdx.x] = float2{__int_as_float(lim), far ? __uint_as_float((uint32_t)min(max(E, 1), 253) << 23) : 1.0f};
       scaled |= far;
       float sq[NG];
 #pragma unroll
@@ -866,8 +945,10 @@ __global__ __launch_bounds__(64 * WV, 2) void page_prompt_kernel(PageAttendArgs 
       }
       sqb[c] = u4{bits[0], bits[1], bits[2], bits[3]};
     }
-    scaled = __builtin_amdgcn_ballot_w64(scaled) != 0;
-    const int lim_all = (int)max((int64_t)0, (int64_t)x.len - x.n + (int64_t)b * QROWS / G + 1);
+    const bool always = __builtin_amdgcn_ballot_w64(scaled) != 0;
+    // rows below it are seen by all of the wave's queries
+    const int lim_all =
+        (int)max((int64_t)0, (int64_t)x.len - x.n + min((int64_t)b * QROWS + wave * 32, (int64_t)x.n * G - 1) / G + 1);
 
     float m[2] = {kNone, kNone}, l[2] = {0.0f, 0.0f};
     f4 acc[2][DT], low[2];
@@ -879,110 +960,157 @@ __global__ __launch_bounds__(64 * WV, 2) void page_prompt_kernel(PageAttendArgs 
     }
 
     if (x.len > 0) {
-      stage(tiles_lds[0]);
-      if (t0 + 1 < t1) issue(t0 + 1);
-      for (int t = t0; t < t1; ++t) {
-        PromptTile<D>& L = tiles_lds[(t - t0) & 1];
-        __syncthreads();  // this tile is whole, and the other one is no longer read
-        if (t + 1 < t1) stage(tiles_lds[(t - t0 + 1) & 1]);
-        if (t + 2 < t1) issue(t + 2);
-
-        // products with keys 16 k + 4 g4 + j
-        f4 sc[2][4];
+      // products of both blocks of queries with 16 keys
+      auto products = [&](const Keys& L, int first, f4& s0, f4& s1) {
+        const u4 km = *reinterpret_cast<const u4*>(&L.m[first + i16][0]);
+        s0 = mfma_f16(km, sqb[0], f4{0.f, 0.f, 0.f, 0.f});
+        s1 = mfma_f16(km, sqb[1], f4{0.f, 0.f, 0.f, 0.f});
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const u4 km = *reinterpret_cast<const u4*>(&L.km[k * 16 + i16][0]);
-          sc[0][k] = mfma_f16(km, sqb[0], f4{0.f, 0.f, 0.f, 0.f});
-          sc[1][k] = mfma_f16(km, sqb[1], f4{0.f, 0.f, 0.f, 0.f});
-#pragma unroll
-          for (int st = 0; st < KS; ++st) {
-            const u4 ka = *reinterpret_cast<const u4*>(L.k + (k * 16 + i16) * kRow<D> + (st * 4 + g4) * 16);
-            sc[0][k] = mfma_f16(ka, qb[0][st], sc[0][k]);
-            sc[1][k] = mfma_f16(ka, qb[1][st], sc[1][k]);
-          }
+        for (int st = 0; st < KS; ++st) {
+          const u4 ka = *reinterpret_cast<const u4*>(L.k + (first + i16) * kRow<D> + (st * 4 + g4) * 16);
+          s0 = mfma_f16(ka, qb[0][st], s0);
+          s1 = mfma_f16(ka, qb[1][st], s1);
         }
-        if (scaled) {
-          asm volatile("");
+      };
+      // weights of 32 keys for queries c: w = 2^(logit + e - m); their sum,
+      // and that of l
+      auto weigh = [&](const Keys& K, const Values& V, int sub, int c, const f4& s0, const f4& s1, float& sum,
+                       float& sum_l) {
+        float e[8], part[2];
 #pragma unroll
-          for (int c = 0; c < 2; ++c)
+        for (int i = 0; i < 2; ++i) {
+          const float kf = K.f[sub * 2 + i], off = V.e[sub * 2 + i] - m[c];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) sc[c][k] *= qf[c];
+          for (int j = 0; j < 4; ++j) e[i * 4 + j] = __builtin_amdgcn_exp2f(fmaf(i ? s1[j] : s0[j], kf, off));
+          part[i] = (e[i * 4] + e[i * 4 + 1]) + (e[i * 4 + 2] + e[i * 4 + 3]);
         }
-        // logits and the values' exponents
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const f4 kf = *reinterpret_cast<const f4*>(&L.kf[k * 16 + g4 * 4]);
-          const f4 ve = *reinterpret_cast<const f4*>(&L.ve[k * 16 + g4 * 4]);
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            sc[0][k][j] = fmaf(sc[0][k][j], kf[j], ve[j]);
-            sc[1][k][j] = fmaf(sc[1][k][j], kf[j], ve[j]);
-          }
-        }
-        const int r0 = t * KT;
-        if (r0 + KT > lim_all) {
-          asm volatile("");
-#pragma unroll
-          for (int c = 0; c < 2; ++c)
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-#pragma unroll
-              for (int j = 0; j < 4; ++j)
-                if (r0 + k * 16 + g4 * 4 + j >= lim[c]) sc[c][k][j] = -INFINITY;
-        }
-#pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          float mx = -INFINITY;
-#pragma unroll
-          for (int k = 0; k < 4; ++k)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) mx = fmaxf(mx, sc[c][k][j]);
-          if (__builtin_amdgcn_ballot_w64(mx > m[c] + kLazy)) {
-            mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
-            mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-            const float m_new = fmaxf(m[c], mx), alpha = __builtin_amdgcn_exp2f(m[c] - m_new);
-            m[c] = m_new;
-            l[c] *= alpha;
-            low[c] *= alpha;
-#pragma unroll
-            for (int d = 0; d < DT; ++d) acc[c][d] *= alpha;
-          }
-        }
-        u4 p[2][2];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const f4 vi = *reinterpret_cast<const f4*>(&L.vi[k * 16 + g4 * 4]);
-#pragma unroll
-          for (int c = 0; c < 2; ++c) {
-            float e[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              e[j] = __builtin_amdgcn_exp2f(sc[c][k][j] - m[c]);
-              l[c] = fmaf(e[j], vi[j], l[c]);
-            }
-            p[c][k >> 1][2 * (k & 1)] = h2(e[0], e[1]);
-            p[c][k >> 1][2 * (k & 1) + 1] = h2(e[2], e[3]);
-          }
-        }
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          const _Float16* vm = &L.vm[i16 & (NG - 1)][half * 32 + g4 * 4];
+        sum = part[0] + part[1];
+        sum_l = fmaf(part[0], V.inv[sub * 2], part[1] * V.inv[sub * 2 + 1]);
+        return u4{h2(e[0], e[1]), h2(e[2], e[3]), h2(e[4], e[5]), h2(e[6], e[7])};
+      };
+      auto output = [&](const Values& L, int sub, const u4 (&p)[2], int d0, int d1) {
+        if (d0 == 0) {
+          const _Float16* vm = &L.m[i16 & (NG - 1)][sub * 32 + g4 * 4];
           const uint2 v0 = *reinterpret_cast<const uint2*>(vm), v1 = *reinterpret_cast<const uint2*>(vm + 16);
           const u4 va{v0.x, v0.y, v1.x, v1.y};
-          low[0] = mfma_f16(va, p[0][half], low[0]);
-          low[1] = mfma_f16(va, p[1][half], low[1]);
-          const char* vb = (const char*)L.v + (half * 32 + g4 * 4 + (i16 >> 2)) * kRow<D> + (i16 & 3) * 8;
-#pragma unroll
-          for (int d = 0; d < DT; ++d) {
-            const u4 vt = ds_tr(vb + d * 32, vb + 16 * kRow<D> + d * 32);
-            acc[0][d] = mfma_f16(vt, p[0][half], acc[0][d]);
-            acc[1][d] = mfma_f16(vt, p[1][half], acc[1][d]);
-          }
+          low[0] = mfma_f16(va, p[0], low[0]);
+          low[1] = mfma_f16(va, p[1], low[1]);
         }
+        const char* vb = (const char*)L.v + (sub * 32 + g4 * 4 + (i16 >> 2)) * kRow<D> + (i16 & 3) * 8;
+#pragma unroll
+        for (int d = d0; d < d1; ++d) {
+          const u4 vt = ds_tr(vb + d * 32, vb + 16 * kRow<D> + d * 32);
+          acc[0][d] = mfma_f16(vt, p[0], acc[0][d]);
+          acc[1][d] = mfma_f16(vt, p[1], acc[1][d]);
+        }
+      };
+
+      const int stages = (t1 - t0) * (KT / KEYS);
+      // keys of stages 0 and 1, values of stage 0; the thread then holds its
+      // share of the keys of stage 2 or of the values of stage 1
+      if (kind == 0) {
+        store_keys(keys[0]);
+        issue(1);
+        store_keys(keys[1]);
+        issue(2);
+      } else if (kind == 1) {
+        store_values(values[0]);
+        issue(1);
       }
+      __syncthreads();
+      f4 sc[2][2];
+      u4 p[2] = {u4{0, 0, 0, 0}, u4{0, 0, 0, 0}};
+      products(keys[0], 0, sc[0][0], sc[1][0]);
+      products(keys[0], 16, sc[0][1], sc[1][1]);
+      int k0 = 0, k1 = 1, k2 = 2;  // slots of the stage at hand, the next and the one after
+      int vp = 0, v0 = 0, v1 = 1;  // the one before (at first: any with finite values), at hand, the next
+      for (int n = 0; n < stages; ++n) {
+        __syncthreads();
+        // a SIMD's two waves stage at different times
+        if (kind == 0) {
+          store_keys(keys[k2]);
+          issue(n + 3);
+        }
+#pragma unroll 1
+        for (int sub = 0; sub < SPS; ++sub) {
+          if (sub == SPS - 1 && kind == 1) {
+            store_values(values[v1]);
+            issue(n + 2);
+          }
+          const Keys& K = keys[k0];
+          const Values& V = values[v0];
+          const Keys& Kn = keys[sub + 1 < SPS ? k0 : k1];
+          const Values& Vp = values[sub == 0 ? vp : v0];
+          const int next = sub + 1 < SPS ? sub + 1 : 0, prev = sub == 0 ? SPS - 1 : sub - 1;
+          const int before_sub = n == 0 && sub == 0 ? 0 : prev;
+          float sum[2], top[2];
+          u4 pn[2];
+          pn[0] = weigh(K, V, sub, 0, sc[0][0], sc[0][1], top[0], sum[0]);
+          pn[1] = weigh(K, V, sub, 1, sc[1][0], sc[1][1], top[1], sum[1]);
+          products(Kn, next * 32, sc[0][0], sc[1][0]);
+          products(Kn, next * 32 + 16, sc[0][1], sc[1][1]);
+          output(Vp, before_sub, p, 0, DT);
+          const int r0 = t0 * KT + n * KEYS + sub * 32;
+          const bool mask = always || r0 + 32 > lim_all;
+          if (__builtin_amdgcn_ballot_w64(mask || !(top[0] <= 256.0f && top[1] <= 256.0f))) {
+            // rare: the step's products again (its keys are still there),
+            // masked, against a reference raised where it has to be
+            f4 s2[2][2];
+            products(K, sub * 32, s2[0][0], s2[1][0]);
+            products(K, sub * 32 + 16, s2[0][1], s2[1][1]);
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+              const float2 lq = s_rows[c][threadIdx.x];  // the first row not seen, the power taken out
+              const int lim = __float_as_int(lq.x);
+              float mx = -INFINITY;
+#pragma unroll
+              for (int i = 0; i < 2; ++i) {
+                const float kf = K.f[sub * 2 + i], ve = V.e[sub * 2 + i];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                  s2[c][i][j] = fmaf(s2[c][i][j] * lq.y, kf, ve);
+                  if (r0 + i * 16 + g4 * 4 + j >= lim) s2[c][i][j] = -INFINITY;
+                  mx = fmaxf(mx, s2[c][i][j]);
+                }
+              }
+              mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+              mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+              if (mx > m[c] + 5.0f) {  // (eight weights above 256 together: one above 2^5)
+                const float alpha = __builtin_amdgcn_exp2f(m[c] - mx);
+                m[c] = mx;
+                l[c] *= alpha;
+                low[c] *= alpha;
+#pragma unroll
+                for (int d = 0; d < DT; ++d) acc[c][d] *= alpha;
+              }
+              float e[8];
+              sum[c] = 0.0f;
+#pragma unroll
+              for (int i = 0; i < 2; ++i) {
+                const float vi = V.inv[sub * 2 + i];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                  e[i * 4 + j] = __builtin_amdgcn_exp2f(s2[c][i][j] - m[c]);
+                  sum[c] = fmaf(e[i * 4 + j], vi, sum[c]);
+                }
+              }
+              pn[c] = u4{h2(e[0], e[1]), h2(e[2], e[3]), h2(e[4], e[5]), h2(e[6], e[7])};
+            }
+          }
+          l[0] += sum[0];
+          l[1] += sum[1];
+          p[0] = pn[0];
+          p[1] = pn[1];
+        }
+        const int ko = k0, vo = n == 0 ? 2 : vp;  // the slots that fall free
+        k0 = k1, k1 = k2, k2 = ko;
+        vp = v0, v0 = v1, v1 = vo;
+      }
+      output(values[vp], SPS - 1, p, 0, DT);
     }
 
     const int any_bad = __syncthreads_or(bad);
+    if (threadIdx.x == 0 && s_wide) wide[blockIdx.x] = 1;
     const bool begins = before >= u0, ends = before + tiles <= u1;
     float* out = record<D, QROWS>(rec, w, Hkv, h, begins);
 #pragma unroll
@@ -992,6 +1120,8 @@ __global__ __launch_bounds__(64 * WV, 2) void page_prompt_kernel(PageAttendArgs 
       ls += __shfl_xor(ls, 32, 64);
       if (any_bad) ls = __builtin_nanf("");
       const int r = wave * 32 + c * 16 + i16;
+      const int rr = b * QROWS + min(r, rows - 1);
+      const int64_t tok = (int64_t)(x.q0 + rr / G) * Hq + h * G + rr % G;  // among the rows of o
       const float inv = begins && ends ? (ls == 0.0f ? 0.0f : 1.0f / ls) : 1.0f;
       const bool odd = g4 & 1;
 #pragma unroll
@@ -1005,14 +1135,14 @@ __global__ __launch_bounds__(64 * WV, 2) void page_prompt_kernel(PageAttendArgs 
         if (r >= rows) continue;
         if (begins && ends) {
           const uint2 v = q_f16 ? uint2{h2(z[0], z[1]), h2(z[2], z[3])} : uint2{bf2(z[0], z[1]), bf2(z[2], z[3])};
-          *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.o) + tok[c] * D + d * 16 + g4 * 4) = v;
+          *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.o) + tok * D + d * 16 + g4 * 4) = v;
         } else {
           *reinterpret_cast<f4*>(out + r * kRec<D> + d * 16 + g4 * 4) = z;
         }
       }
       if (g4 == 0 && r < rows) {
         if (begins && ends) {
-          if (a.lse) a.lse[tok[c]] = lse_of(m[c], ls);
+          if (a.lse) a.lse[tok] = lse_of(m[c], ls);
         } else {
           out[r * kRec<D> + D] = m[c];
           out[r * kRec<D> + D + 1] = ls;
@@ -1027,31 +1157,28 @@ __global__ __launch_bounds__(64 * WV, 2) void page_prompt_kernel(PageAttendArgs 
       b = 0;
       do {
         if (++s >= a.S) return;
-        x = seq_of(a, s);
-        nb = prompt_blocks<WV>(x, G);
+        x = scalar(seq_of(a, s));
+        nb = prompt_blocks(x, G);
       } while (nb == 0);
     }
   }
 }
 
-// One workgroup per cut and group of its rows: its pieces' records in order,
-// ROWS query rows from row `block` of the sequence on.  A thread takes four
-// channels; a row's references and sums come first, so that the records' loads
-// do not wait for one another.
+// A cut's pieces' records in order: ROWS query rows from row `block` of the
+// sequence on, those that fall to workgroup y of `ys`.  A thread takes four
+// channels; the loads of a few records do not wait for one another.
 template <int D, int ROWS, int QT>
-__global__ __launch_bounds__(256) void page_merge_kernel(PageAttendArgs a, const float* __restrict__ rec,
-                                                         const Cut* __restrict__ cuts) {
-  const Cut k = cuts[blockIdx.x];
-  if (k.seq < 0) return;
-  const int Hkv = a.pc.Hkv, h = blockIdx.x % Hkv, G = a.G, Hq = G * Hkv;
+__device__ inline void merge_cut(const PageAttendArgs& a, const Cut& k, int h, const float* __restrict__ rec, int y0,
+                                 int ys) {
+  const int Hkv = a.pc.Hkv, G = a.G, Hq = G * Hkv;
   const Seq x = seq_of(a, k.seq);
   const int rows = (int)min((int64_t)ROWS, (int64_t)x.n * G - k.block);
   constexpr int TR = D / 4;  // threads of a row
   const int d = threadIdx.x % TR * 4;
-  for (int r = blockIdx.y * (256 / TR) + threadIdx.x / TR; r < rows; r += gridDim.y * (256 / TR)) {
+  for (int r = y0 * (256 / TR) + threadIdx.x / TR; r < rows; r += ys * (256 / TR)) {
     float M = kNone, l = 0.0f;
     f4 y = f4{0.f, 0.f, 0.f, 0.f};
-    constexpr int N = 8;  // records at a time
+    constexpr int N = 6;  // records at a time
     for (int w0 = k.first; w0 <= k.last; w0 += N) {
       f4 v[N];
       float m[N], ls[N];
@@ -1088,52 +1215,107 @@ __global__ __launch_bounds__(256) void page_merge_kernel(PageAttendArgs a, const
   }
 }
 
+// the rows of a block that fall to workgroup y0 of `ys`, from the cache itself
+template <int D, int QT>
+__device__ inline void attend_block(const PageAttendArgs& a, RowLds<D>& lds, int s, int block, int h, int y0, int ys) {
+  const Seq x = seq_of(a, s);
+  const int rows = (int)min((int64_t)QROWS, (int64_t)x.n * a.G - block);
+  for (int r = block + y0; r < block + rows; r += ys)
+    attend_row<D, QT>(a, lds, x, s, x.q0 + r / a.G, h * a.G + r % a.G);
+}
+
+// Cuts of the token kernel (blocks [0, n_tokens) of the grid) and of the prompt
+// kernel (those behind).  Blocks that a piece marked as wide has a part in are
+// computed anew, whole ones of the piece by its own workgroups.
+template <int D, int QT>
+__global__ __launch_bounds__(256, 8) void page_merge_kernel(PageAttendArgs a, int n_tokens, const Cut* __restrict__ cuts_t,
+                                                         const float* __restrict__ rec_t,
+                                                         const Cut* __restrict__ cuts_p,
+                                                         const float* __restrict__ rec_p, int Wp,
+                                                         const int* __restrict__ units, const int* __restrict__ wide) {
+  if ((int)blockIdx.x < n_tokens) {
+    if (blockIdx.y >= 2) return;
+    const Cut k = cuts_t[blockIdx.x];
+    if (k.seq >= 0) merge_cut<D, 16, QT>(a, k, blockIdx.x % a.pc.Hkv, rec_t, blockIdx.y, min((int)gridDim.y, 2));
+    return;
+  }
+  __shared__ RowLds<D> lds;
+  const int i = blockIdx.x - n_tokens, Hkv = a.pc.Hkv, h = i % Hkv, w = i / Hkv;
+  const Cut k = cuts_p[i];
+  const int all = wide[i];
+  if (k.seq >= 0) {
+    int any = 0;
+    for (int j = k.first + threadIdx.x; j <= k.last; j += blockDim.x) any |= wide[j * Hkv + h];
+    if (__syncthreads_or(any)) attend_block<D, QT>(a, lds, k.seq, k.block, h, blockIdx.y, gridDim.y);
+    else merge_cut<D, QROWS, QT>(a, k, h, rec_p, blockIdx.y, gridDim.y);
+  }
+  if (!all) return;
+  const int U = units[a.S];
+  const Line line(U, min(Wp, U));
+  const int u0 = line.first(w), u1 = line.first(w + 1);
+  for (int s = 0; s < a.S; ++s) {
+    if (units[s + 1] <= u0 || units[s] >= u1) continue;
+    const Seq x = seq_of(a, s);
+    int before = units[s];
+    for (int b = 0; b < prompt_blocks(x, a.G) && before < u1; ++b) {
+      const int tiles = prompt_tiles(x, a.G, b);
+      if (before >= u0 && before + tiles <= u1) attend_block<D, QT>(a, lds, s, b * QROWS, h, blockIdx.y, gridDim.y);
+      before += tiles;
+    }
+  }
+}
+
 }  // namespace
 
-// pieces of the line per KV head: two workgroups per CU in one round
-static int pieces(const PageCache& pc) { return std::max(1, 2 * device_cus() / pc.Hkv); }
+// Pieces of the line per KV head: two workgroups per CU in one round for
+// single tokens, one (of twice the waves) for prompts.
+static int token_pieces(const PageCache& pc) { return std::max(1, 2 * device_cus() / pc.Hkv); }
+static int prompt_pieces(const PageCache& pc) { return std::max(1, device_cus() / pc.Hkv); }
 
 static size_t align_up(size_t x) { return (x + 255) & ~(size_t)255; }
 
-// cuts, the prompt kernel's sums of units, records (none where there is one
-// piece); the two kernels of a call use it one after the other
-static size_t records_at(const PageCache& pc, int S) {
-  return align_up((size_t)pieces(pc) * pc.Hkv * sizeof(Cut)) + align_up(((size_t)S + 1) * sizeof(int));
-}
-
-// eight waves a workgroup where blocks of 256 rows are well filled
-static bool wide_prompt(int max_q, int G) { return (int64_t)max_q * G >= 512; }
+// cuts and records of both kernels (no records where there is one piece), the
+// prompt kernel's sums of units and marks
+struct PageWorkspace {
+  size_t cuts_p, wide, units, rec_t, rec_p, end;
+  PageWorkspace(const PageCache& pc, int S, bool prompts) {
+    const size_t nt = (size_t)token_pieces(pc) * pc.Hkv, np = (size_t)prompt_pieces(pc) * pc.Hkv;
+    cuts_p = align_up(nt * sizeof(Cut));
+    wide = cuts_p + (prompts ? align_up(np * sizeof(Cut)) : 0);
+    units = wide + (prompts ? align_up(np * sizeof(int)) : 0);
+    rec_t = units + (prompts ? align_up(((size_t)S + 1) * sizeof(int)) : 0);
+    const size_t row = (pc.D + 4) * sizeof(float);
+    rec_p = rec_t + (nt > (size_t)pc.Hkv ? nt * 2 * 16 * row : 0);
+    end = rec_p + (prompts && np > (size_t)pc.Hkv ? np * 2 * QROWS * row : 0);
+  }
+};
 
 size_t page_attend_workspace(const PageCache& pc, int G, int S, int max_q) {
-  const size_t W = pieces(pc);
-  if (W == 1) return records_at(pc, S);
-  // (prompts: half the workgroups where they have twice the rows)
-  const size_t rows = (int64_t)max_q * G <= 16 ? 16 : kQRows<4>;
-  return records_at(pc, S) + W * pc.Hkv * 2 * rows * (pc.D + 4) * sizeof(float);
+  return PageWorkspace(pc, S, (int64_t)max_q * G > 16).end;
 }
 
 template <int D, int NG, int QP>
 static void launch_matrix(const PageAttendArgs& a, int max_q, void* ws, hipStream_t st) {
   constexpr int QT = QP == 1 ? UC_BF16 : UC_F16;
-  const int W = pieces(a.pc);
-  Cut* cuts = (Cut*)ws;
-  int* units = (int*)((char*)ws + align_up((size_t)W * a.pc.Hkv * sizeof(Cut)));
-  float* rec = (float*)((char*)ws + records_at(a.pc, a.S));
-  const int64_t most = a.S * std::max<int64_t>(1, (((int64_t)a.ld << a.pc.lgP) + KT - 1) / KT);  // tiles there can be
-  const int Wt = (int)std::max<int64_t>(1, std::min<int64_t>(W, (most + (int64_t)kStart * a.S) / (kStart + WAVES))), n = Wt * a.pc.Hkv;
-  hipLaunchKernelGGL((page_tokens_kernel<D, NG, QP>), dim3(n), dim3(256), 0, st, a, Wt, rec, cuts);
-  if (Wt > 1) hipLaunchKernelGGL((page_merge_kernel<D, 16, QT>), dim3(n, 2), dim3(256), 0, st, a, rec, cuts);
-  if ((int64_t)max_q * a.G <= 16) return;
-  auto prompts = [&](auto waves) {
-    constexpr int WV = decltype(waves)::value;
-    const int Wp = W * 4 / WV > 1 ? W * 4 / WV : 1, np = Wp * a.pc.Hkv;  // workgroups of WV waves: two waves per SIMD
-    hipLaunchKernelGGL(page_plan_kernel<WV>, dim3(1), dim3(1024), 0, st, a, units);
-    hipLaunchKernelGGL((page_prompt_kernel<D, NG, WV>), dim3(np), dim3(64 * WV), 0, st, a, Wp, QP == 2, units, rec, cuts);
-    if (Wp > 1)
-      hipLaunchKernelGGL((page_merge_kernel<D, kQRows<WV>, QT>), dim3(np, 16), dim3(256), 0, st, a, rec, cuts);
-  };
-  if (wide_prompt(max_q, a.G)) prompts(std::integral_constant<int, 8>{});
-  else prompts(std::integral_constant<int, 4>{});
+  const bool prompts = (int64_t)max_q * a.G > 16;
+  const PageWorkspace at(a.pc, a.S, prompts);
+  char* p = (char*)ws;
+  Cut *cuts_t = (Cut*)p, *cuts_p = (Cut*)(p + at.cuts_p);
+  int *units = (int*)(p + at.units), *wide = (int*)(p + at.wide);
+  float *rec_t = (float*)(p + at.rec_t), *rec_p = (float*)(p + at.rec_p);
+  // no more pieces than there can be work for
+  const int64_t most = a.S * (kStart + std::max<int64_t>(1, (((int64_t)a.ld << a.pc.lgP) + KT - 1) / KT));
+  const int Wt = (int)std::max<int64_t>(1, std::min<int64_t>(token_pieces(a.pc), most / (kStart + WAVES)));
+  const int nt = Wt * a.pc.Hkv, Wp = prompt_pieces(a.pc), np = prompts ? Wp * a.pc.Hkv : 0;
+  hipLaunchKernelGGL((page_tokens_kernel<D, NG, QP>), dim3(nt + (prompts ? 1 : 0)), dim3(256), 0, st, a, Wt, rec_t,
+                     cuts_t, units);
+  if (prompts)
+    hipLaunchKernelGGL((page_prompt_kernel<D, NG>), dim3(np), dim3(64 * PWAVES), 0, st, a, Wp, QP == 2, units, rec_p,
+                       cuts_p, wide);
+  const int merge_t = Wt > 1 ? nt : 0, merge_p = np;
+  if (merge_t + merge_p)
+    hipLaunchKernelGGL((page_merge_kernel<D, QT>), dim3(merge_t + merge_p, merge_p ? 16 : 2), dim3(256), 0, st, a,
+                       merge_t, cuts_t, rec_t, cuts_p, rec_p, Wp, units, wide);
 }
 
 hipError_t launch_page_valu(const PageAttendArgs& a, int q_dt, hipStream_t st) {

@@ -127,6 +127,34 @@ def attend(cache, q, q_start, lens, table, scale):
     return o, lse
 
 
+def sizes(cache, q, q_start, lens, table, scale, lse, unit):
+    """What a row's errors are measured by: sum_j p_j M_j per channel, with M_j
+    the largest size in the channel's group of value j, and the same sums of
+    d_j (lse's error) and d_j M_j, where d_j = unit * scale * sum |q| M'_j, M'_j
+    likewise of key j, is the error of a logit and p_j is taken with it."""
+    T, Hq, D = q.shape
+    G = Hq // cache.Hkv
+    size, d_size, d_lse = np.zeros((T, Hq, D)), np.zeros((T, Hq, D)), np.zeros((T, Hq))
+    for s, n_rows in enumerate(lens):
+        a, b = int(q_start[s]), int(q_start[s + 1])
+        if b <= a or n_rows == 0:
+            continue
+        k, v = cache.rows(slots_of(table[s], n_rows, cache.P))
+        most = []
+        for x in (k, v):
+            g = np.abs(x).reshape(n_rows, cache.Hkv, D // cache.group, cache.group)
+            most.append(np.broadcast_to(g.max(-1, keepdims=True), g.shape).reshape(x.shape))
+        for i in range(b - a):
+            sees = max(0, n_rows - (b - a) + i + 1)
+            for h in range(Hq if sees else 0):
+                x = k[:sees, h // G] @ q[a + i, h] * scale
+                d = most[0][:sees, h // G] @ np.abs(q[a + i, h]) * scale * unit
+                p = np.exp(np.minimum(x + d - lse[a + i, h], 0))
+                size[a + i, h], d_lse[a + i, h] = p @ most[1][:sees, h // G], p @ d
+                d_size[a + i, h] = (p * np.minimum(d, 1)) @ most[1][:sees, h // G]
+    return size, d_size, d_lse
+
+
 def free_pages(table, lens, P, n_pages):
     held = {int(p) for row, n in zip(table, lens) for p in row[:min(-(-max(int(n), 0) // P), len(row))]}
     return [p for p in range(n_pages) if p not in held]

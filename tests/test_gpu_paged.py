@@ -302,6 +302,109 @@ def test_sharp_logits(tokens):
     assert np.allclose(f64(lse), lse_ref, rtol=1e-5, atol=1e-4)
 
 
+def put_rows(cache, table, s, at, k, v):
+    """Rows of k and v [n, Hkv, D] as rows `at` of sequence s."""
+    cache.append(k.astype(np.float32), v.astype(np.float32), [ref.slots_of(table[s], j + 1, cache.P)[-1] for j in at])
+
+
+def check_sized(cache, q, start, lens, table, scale, o, lse, dtype):
+    """Against 64 bits, with bounds by what adds up to a row.
+
+    A logit is a sum of D terms in binary32, off by D 2^-24 of the sum of their
+    sizes.  A term is at most |q| M, M the largest size in its group of the
+    key; single tokens sum (128 + code) s q instead, with s <= 2 M / 15 * 9/8
+    at most 22 times as much.  lse is off by the logits' errors weighed by
+    their keys, beside 1e-5 of itself and 2^-12.
+
+    An output is off by twice the logits' errors, by its own rounding (in fp16
+    2^-25 where it is subnormal) and by what its terms are rounded by.  Prompts:
+    weights in fp16, 2^-12, and a minimum, within 2^-12 of its step.  Single
+    tokens: p s in two bf16 parts, each within 2^-9 of what it rounds, times
+    128 + code: 143 * 2^-18 s, 2^-13.5 of M.  2^-11 of the sum of p M covers
+    both."""
+    want, want_lse = ref.attend(cache, f64(q), start, lens, table, scale)
+    for s, n in enumerate(np.diff(start)):
+        at = slice(start[s], start[s + 1])
+        few = n * (q.shape[1] // cache.Hkv) <= 16
+        size, d_size, d_lse = (x[at] for x in ref.sizes(cache, f64(q), start, lens, table, scale, want_lse,
+                                                        cache.D * 2.0 ** -24 * (22 if few else 1)))
+        tiny = 2.0 ** -25 if dtype == "f16" else 2.0 ** -126
+        bound = half(dtype) * np.abs(want[at]) + 2.0 ** -11 * size + 2 * d_size + tiny
+        bad = ~(np.abs(f64(o[at]) - want[at]) <= bound)
+        assert not bad.any(), (s, np.argwhere(bad)[:4], f64(o[at])[bad][:4], want[at][bad][:4], bound[bad][:4])
+        bound = 2.0 ** -12 + 1e-5 * np.abs(want_lse[at]) + d_lse
+        bad = ~(np.abs(f64(lse[at]) - want_lse[at]) <= bound)
+        assert not bad.any(), (s, np.argwhere(bad)[:4], f64(lse[at])[bad][:4], want_lse[at][bad][:4], bound[bad][:4])
+
+
+FAR = {  # name: (factor of keys, of values) of the rows named
+    "keys_large": ([37, 38, 290], 2.0 ** 30, 1.0),
+    "keys_small": ([0, 1, 2, 3, 70, 290], 2.0 ** -40, 1.0),
+    "values_large": ([37, 38, 290], 1.0, 2.0 ** 30),
+    "values_small": ([0, 1, 2, 3, 70, 290], 1.0, 2.0 ** -40),
+    "all_values_large": (range(320), 1.0, 2.0 ** 84),
+    "all_values_small": (range(320), 1.0, 2.0 ** -70),
+    "all_keys_small": (range(320), 2.0 ** -110, 1.0),
+    "both_ends": (range(16, 32), 2.0 ** 14, 2.0 ** -16),
+}
+
+
+@pytest.mark.parametrize("group", [32, 128])
+@pytest.mark.parametrize("tokens", [2, 150, 320])
+@pytest.mark.parametrize("name", list(FAR))
+def test_rows_of_far_sizes(name, tokens, group):
+    _case(test="far", name=name, tokens=tokens, group=group)
+    at, fk, fv = FAR[name]
+    lens, Hkv, G, D = [320, 90], 2, 4, 128
+    cache, table = make_cache(lens, 16, Hkv, D, group, 61)
+    r = np.random.default_rng(62)
+    n = len(at)
+    put_rows(cache, table, 0, at, r.standard_normal((n, Hkv, D)) * fk, r.standard_normal((n, Hkv, D)) * fv)
+    start = [0, tokens, tokens + 2]
+    q = torch.tensor(r.standard_normal((tokens + 2, Hkv * G, D)), device="cuda").to(torch.bfloat16)
+    o, lse = torch.empty_like(q), torch.empty(tokens + 2, Hkv * G, device="cuda")
+    uc.uc_page_attend(cache.device(uc), q, i32(start), i32(lens), i32(table), tokens, 0.1, o, lse)
+    check_sized(cache, q, start, lens, table, float(np.float32(0.1)), o, lse, "bf16")
+
+
+@pytest.mark.parametrize("D,group", [(64, 32), (128, 32), (128, 64)])
+@pytest.mark.parametrize("tokens", [3, 130])
+def test_infinite_rows_that_earlier_queries_do_not_see(tokens, D, group):
+    """A row of infinities spoils no query before it."""
+    _case(test="inf", tokens=tokens, D=D, group=group)
+    lens, Hkv, G = [400, 130], 2, 4
+    cache, table = make_cache(lens, 32, Hkv, D, group, 63)
+    for s, n in enumerate(lens):
+        x = np.zeros((1, Hkv, D), np.float32)
+        x[..., ::3], x[..., 1::3] = np.inf, -np.inf
+        put_rows(cache, table, s, [n - 2], x, x)
+    start = [0, tokens, 2 * tokens]
+    q = torch.randn(2 * tokens, Hkv * G, D, device="cuda").to(torch.bfloat16)
+    o, lse = torch.empty_like(q), torch.empty(2 * tokens, Hkv * G, device="cuda")
+    uc.uc_page_attend(cache.device(uc), q, i32(start), i32(lens), i32(table), tokens, 0.1, o, lse)
+    want, want_lse = ref.attend(cache, f64(q), start, lens, table, float(np.float32(0.1)))
+    for a in start[:2]:
+        b = a + tokens - 2
+        check(o[a:b], lse[a:b], want[a:b], want_lse[a:b], "bf16")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("tokens", [4, 70])
+def test_queries_of_far_sizes(tokens, dtype):
+    """Queries whose sizes differ by powers of two, one of zeros among them."""
+    lens, Hkv, G, D = [257], 2, 2, 128
+    cache, table = make_cache(lens, 16, Hkv, D, 64, 64)
+    r = np.random.default_rng(65)
+    f = 2.0 ** r.integers(-12, 4, (tokens, Hkv * G, 1))
+    f[1] = 0
+    q = r.standard_normal((tokens, Hkv * G, D)) * f
+    q[2], q[3] = q[2] * 2.0 ** 8, q[3] * 2.0 ** -13
+    q = torch.tensor(q, device="cuda").to(DT[dtype])
+    o, lse = torch.empty_like(q), torch.empty(tokens, Hkv * G, device="cuda")
+    uc.uc_page_attend(cache.device(uc), q, i32([0, tokens]), i32(lens), i32(table), tokens, 0.01, o, lse)
+    check_sized(cache, q, [0, tokens], lens, table, float(np.float32(0.01)), o, lse, dtype)
+
+
 @pytest.mark.parametrize("path", ["auto", "valu"])
 @pytest.mark.parametrize("tokens", [1, 24])
 def test_pages_outside_the_cache(tokens, path):
