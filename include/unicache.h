@@ -661,14 +661,14 @@ uc_status uc_page_step(int S, int page_rows, int n_pages, const int32_t* len, co
  * passed over; no slot may occur twice.  copies, when n_copies > 0, is device
  * int32 [n_copies, 3] as uc_beam_reorder writes it: rows 0 .. rows - 1 of page
  * `from` are copied to page `to` (from < 0: nothing); the same call's slots
- * must not lie in rows that are copied. */
+ * must not lie in rows that are copied.  T <= 2^27, n_copies <= 2^22. */
 uc_status uc_page_append(const uc_page_cache* cache, const void* k_new, const void* v_new,
                          uc_dtype dt, int64_t ld, int T, const int32_t* slots,
                          const int32_t* copies, int n_copies, void* stream);
 
 /* The values held in T slots, as dense rows: k_out and v_out at t * ld + h * D
  * in dt (alignment as for uc_page_append).  A slot outside the cache gives
- * zeros. */
+ * zeros.  T <= 2^27. */
 uc_status uc_page_read(const uc_page_cache* cache, const int32_t* slots, int T, void* k_out,
                        void* v_out, uc_dtype dt, int64_t ld, void* stream);
 
@@ -715,8 +715,8 @@ size_t uc_page_attend_workspace_size(const uc_page_cache* cache, int Hq, int T, 
  *   score_out [R, W] float, descending; parent, token [R, W] int32;
  *   done_out  optional uint8 [R, W]: done[parent], or token == eos
  * score_out may be score and done_out may be done.  1 <= W <= UC_MAX_BEAMS,
- * W <= V, W * V < 2^31, 0 <= pad < V; eos may be -1 (none).  Totals are
- * formed in 64 bits from binary32 sums of exponentials.  ws:
+ * W <= V, W * V < 2^31, R * W <= 2^23, 0 <= pad < V; eos may be -1 (none).
+ * Totals are formed in 64 bits from binary32 sums of exponentials.  ws:
  * uc_beam_select_workspace_size bytes. */
 uc_status uc_beam_select(int R, int W, int V, const void* logits, uc_dtype dt, int64_t ld,
                          const float* score, const uint8_t* done, int eos, int pad,

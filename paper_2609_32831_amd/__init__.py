@@ -175,6 +175,9 @@ def _ptr(t: Optional[torch.Tensor]):
     return None if t is None else t.data_ptr()
 
 
+_current = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+
+
 def _stream(stream) -> Optional[int]:
     if stream is None:
         if torch.cuda.is_initialized():
@@ -531,7 +534,7 @@ class PageCache:
                       (scale_v, torch.int32)):
             assert t.dtype == dt and t.is_contiguous() and t.device == codes_k.device
         assert codes_v.shape == codes_k.shape and scale_v.shape == scale_k.shape
-        assert scale_k.shape[:3] == codes_k.shape[:3]
+        assert scale_k.shape[:3] == codes_k.shape[:3] and scale_k.shape[3] > 0
         self.n_pages, self.Hkv, self.page_rows, self.D = n_pages, Hkv, P, 2 * half
         self.group = self.D // scale_k.shape[3]
         self.device, self.at = codes_k.device, codes_k.get_device()
@@ -555,7 +558,8 @@ def page_cache(n_pages: int, page_rows: int, Hkv: int, D: int, group: int = 64,
 
 def _ints(at: int, *ts: Optional[torch.Tensor]):
     """Device int32 tensors, contiguous, on GPU `at`, as the paged calls take
-    them."""
+    them; `at` has to be the current one, where the launches go."""
+    assert at >= 0 and at == _current(), "tensors of the current GPU"
     for t in ts:
         assert t is None or (t.dtype is torch.int32 and t.is_contiguous() and
                              t.get_device() == at), "int32, contiguous, on one device"
@@ -679,7 +683,8 @@ def uc_beam_select(logits: torch.Tensor, score: torch.Tensor, done: Optional[tor
     at, n = logits.get_device(), R * W
     _ints(at, parent, token)
     for t in (score, score_out):
-        assert t.dtype is torch.float32 and t.is_contiguous() and t.get_device() == at
+        assert t.dtype is torch.float32 and t.is_contiguous() and t.get_device() == at, \
+            "scores: float32, contiguous, on the logits' device"
     for t in (done, done_out):
         assert t is None or (t.dtype is torch.uint8 and t.is_contiguous() and t.numel() == n and
                              t.get_device() == at)

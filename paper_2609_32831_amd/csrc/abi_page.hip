@@ -34,6 +34,10 @@ hipError_t launch_beam_reorder(const int32_t* parent, const int32_t* token, cons
 
 namespace {
 
+// rows of an append or a read: 16 or more to a workgroup of 256, of which a
+// launch holds fewer than 2^24
+constexpr int kMostRows = 1 << 27;
+
 bool aligned4(const void* p) { return ((uintptr_t)p & 3u) == 0; }
 
 uc_status check_paging(int page_rows, int64_t n_pages) {
@@ -121,6 +125,7 @@ uc_status uc_page_append(const uc_page_cache* cache, const void* k_new, const vo
   uc_status st = check_cache(cache, pc);
   if (st) return st;
   if (T < 0 || n_copies < 0) return fail(UC_E_INVALID, "T and n_copies must be >= 0 (got %d, %d)", T, n_copies);
+  if (T > kMostRows || n_copies > kMostRows / 32) return fail(UC_E_UNSUPPORTED, "too many rows or copies for one call");
   if (T > 0 && ((st = check_rows("k_new", k_new, dt, ld, (int64_t)pc.Hkv * pc.D)) ||
                 (st = check_rows("v_new", v_new, dt, ld, (int64_t)pc.Hkv * pc.D)) || (st = check_ints("slots", slots))))
     return st;
@@ -135,6 +140,7 @@ uc_status uc_page_read(const uc_page_cache* cache, const int32_t* slots, int T, 
   uc_status st = check_cache(cache, pc);
   if (st) return st;
   if (T < 0) return fail(UC_E_INVALID, "T must be >= 0 (got %d)", T);
+  if (T > kMostRows) return fail(UC_E_UNSUPPORTED, "too many rows for one call");
   if (T == 0 && !dtype_ok(dt)) return fail(UC_E_INVALID, "bad dtype %d", dt);
   if (T > 0 && ((st = check_rows("k_out", k_out, dt, ld, (int64_t)pc.Hkv * pc.D)) ||
                 (st = check_rows("v_out", v_out, dt, ld, (int64_t)pc.Hkv * pc.D)) || (st = check_ints("slots", slots))))
@@ -158,10 +164,11 @@ uc_status uc_page_attend(const uc_page_cache* cache, int Hq, const void* q, uc_d
   if (T < 0 || S < 1 || max_q < 1 || table_ld < 1)
     return fail(UC_E_INVALID, "T must be >= 0, S, max_q and table_ld >= 1 (got %d, %d, %d, %d)", T, S, max_q, table_ld);
   if (!dtype_ok(q_dt)) return fail(UC_E_INVALID, "bad q dtype %d", q_dt);
-  if (!(sm_scale > 0.0f) || !isfinite(sm_scale)) return fail(UC_E_INVALID, "sm_scale must be finite and > 0");
+  if (!(sm_scale > 0.0f) || !isfinite(sm_scale * kLog2e)) return fail(UC_E_INVALID, "sm_scale must be finite and > 0");
   if ((int64_t)T * Hq > INT32_MAX) return fail(UC_E_UNSUPPORTED, "too many query rows");
-  // units of work: tiles of 64 rows, once per 128 query rows
-  const int64_t tiles = ((int64_t)table_ld * cache->page_rows + 63) / 64 + 8;  // (8: what a sequence counts beside them)
+  // units of work: tiles of 64 rows and what a sequence counts beside them,
+  // for every block of 256 query rows, taken as 128
+  const int64_t tiles = ((int64_t)table_ld * cache->page_rows + 63) / 64 + kStart;
   if (tiles > INT32_MAX / 64 || tiles * ((int64_t)S + (int64_t)T * (Hq / pc.Hkv) / 128) > INT32_MAX)
     return fail(UC_E_UNSUPPORTED, "tables of %d pages for %d sequences and %d tokens hold too much work for one call",
                 table_ld, S, T);
@@ -181,7 +188,7 @@ uc_status uc_page_attend(const uc_page_cache* cache, int Hq, const void* q, uc_d
 }
 
 size_t uc_beam_select_workspace_size(int R, int W, int V) {
-  if (R < 1 || W < 1 || W > UC_MAX_BEAMS || V < W || (int64_t)W * V > INT32_MAX || (int64_t)R * W > (1 << 24)) return 0;
+  if (R < 1 || W < 1 || W > UC_MAX_BEAMS || V < W || (int64_t)W * V > INT32_MAX || (int64_t)R * W > (1 << 23)) return 0;
   return beam_select_workspace(R, W, V);
 }
 
@@ -191,7 +198,7 @@ uc_status uc_beam_select(int R, int W, int V, const void* logits, uc_dtype dt, i
   if (R < 1 || W < 1 || W > UC_MAX_BEAMS)
     return fail(UC_E_INVALID, "R %d must be >= 1 and W %d in [1,%d]", R, W, UC_MAX_BEAMS);
   if (V < W || (int64_t)W * V > INT32_MAX) return fail(UC_E_INVALID, "V %d must be at least W, W * V < 2^31", V);
-  if ((int64_t)R * W > (1 << 24)) return fail(UC_E_UNSUPPORTED, "more than 2^24 beams");
+  if ((int64_t)R * W > (1 << 23)) return fail(UC_E_UNSUPPORTED, "more than 2^23 beams");
   if (!dtype_ok(dt)) return fail(UC_E_INVALID, "bad dtype %d", dt);
   if (!logits || ((uintptr_t)logits & (dt == UC_F32 ? 3u : 1u)))
     return fail(UC_E_INVALID, "logits is NULL or not aligned to its type");
@@ -217,6 +224,7 @@ uc_status uc_beam_reorder(int R, int W, const int32_t* parent, const int32_t* to
   if (st) return st;
   if (R < 1 || W < 1 || W > UC_MAX_BEAMS)
     return fail(UC_E_INVALID, "R %d must be >= 1 and W %d in [1,%d]", R, W, UC_MAX_BEAMS);
+  if ((int64_t)R * W > (1 << 23)) return fail(UC_E_UNSUPPORTED, "more than 2^23 beams");
   if (table_ld < 1 || table_ld > (1 << 22)) return fail(UC_E_INVALID, "table_ld %d not in [1,2^22]", table_ld);
   if ((st = check_ints("parent", parent)) || (st = check_ints("table", table)) || (st = check_ints("len", len)) ||
       (st = check_ints("table_out", table_out)) || (st = check_ints("copies", copies)))

@@ -150,18 +150,23 @@ __device__ inline void attend_row(const PageAttendArgs& a, RowLds<D>& L, const S
 template <int D, int QT>
 __global__ __launch_bounds__(256) void page_attend_valu_kernel(PageAttendArgs a) {
   __shared__ RowLds<D> lds;
-  const int Hq = a.pc.Hkv * a.G, hq = blockIdx.x % Hq, t = blockIdx.x / Hq;
-  // the sequence whose tokens include t
   __shared__ int s_seq;
-  if (threadIdx.x == 0) s_seq = INT32_MAX;
-  __syncthreads();
-  for (int s = threadIdx.x; s < a.S; s += blockDim.x) {
-    const Seq x = seq_of(a, s);
-    if (t >= x.q0 && t < x.q0 + x.n) atomicMin(&s_seq, s);
+  const int Hq = a.pc.Hkv * a.G;
+  for (int row = blockIdx.x; row < a.T * Hq; row += gridDim.x) {
+    const int t = row / Hq;
+    // the sequence whose tokens include t
+    __syncthreads();
+    if (threadIdx.x == 0) s_seq = INT32_MAX;
+    __syncthreads();
+    for (int s = threadIdx.x; s < a.S; s += blockDim.x) {
+      const Seq x = seq_of(a, s);
+      if (t >= x.q0 && t < x.q0 + x.n) atomicMin(&s_seq, s);
+    }
+    __syncthreads();
+    const int s = s_seq;
+    if (s < INT32_MAX) attend_row<D, QT>(a, lds, seq_of(a, s), s, t, row % Hq);  // a row of no sequence stays as it was
+    if (row > INT32_MAX - (int)gridDim.x) break;
   }
-  __syncthreads();
-  const int s = s_seq;
-  if (s < INT32_MAX) attend_row<D, QT>(a, lds, seq_of(a, s), s, t, hq);  // a row of no sequence stays as it was
 }
 
 // ---------------------------------------------------------------- the line of tiles
@@ -180,7 +185,6 @@ struct Line {
 // units of a sequence in the single-token kernel: its tiles, at least one so
 // that a row that sees nothing is written too, behind kStart units that stand
 // for what a sequence costs beside them; none where the prompt kernel takes it
-constexpr int kStart = 8;
 __device__ inline int tiles_of(int rows) { return rows <= KT ? 1 : (int)(((uint32_t)rows + KT - 1) / KT); }
 __device__ inline int token_units(const Seq& x, int G) {
   return x.n == 0 || (int64_t)x.n * G > 16 ? 0 : kStart + tiles_of(x.len);
@@ -1319,7 +1323,7 @@ static void launch_matrix(const PageAttendArgs& a, int max_q, void* ws, hipStrea
 }
 
 hipError_t launch_page_valu(const PageAttendArgs& a, int q_dt, hipStream_t st) {
-  const dim3 grid((uint32_t)((int64_t)a.T * a.pc.Hkv * a.G));
+  const dim3 grid(std::min<uint32_t>((uint32_t)a.T * a.pc.Hkv * a.G, 1 << 20));
 #define UC_VALU(DIM, TYPE) \
   hipLaunchKernelGGL((page_attend_valu_kernel<DIM, TYPE>), grid, dim3(256), 0, st, a)
   if (a.pc.D == 128) {

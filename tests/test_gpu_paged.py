@@ -593,6 +593,126 @@ def test_beam_reorder(R, W, P, n, nb, inplace):
         assert len(set(held[:, -1].tolist())) == R * W
 
 
+@pytest.mark.parametrize("R,W,V,dtype", [(3, 32, 70001, "bf16"), (200, 5, 1030, "f16"), (1, 2, 1 << 20, "f32")])
+def test_beam_selection_of_many_beams(R, W, V, dtype):
+    _case(test="beams", R=R, W=W, V=V, dtype=dtype)
+    g = torch.Generator(device="cuda").manual_seed(R + V)
+    x = (torch.randn(R, W, V, generator=g, device="cuda") * 3).to(DT[dtype])
+    score = -torch.rand(R, W, generator=g, device="cuda") * 5
+    done = torch.zeros(R, W, dtype=torch.uint8, device="cuda")
+    check_beams(select(x, score, done, 3, 0), ref.beam_select(f64(x), f64(score), done.cpu().numpy(), 3, 0))
+
+
+# ---------------------------------------------------------------- places
+
+def test_pages_behind_4_gib():
+    """The same rows in a small cache and at the end of one whose codes pass
+    2^32 bytes give the same bits."""
+    lens, tokens, Hkv, D, P, group = [200, 70], [70, 1], 8, 128, 64, 32
+    large = uc.page_cache(140000, P, Hkv, D, group)
+    assert large.t["codes_k"].numel() > 1 << 32
+    small = uc.page_cache(6, P, Hkv, D, group)
+    table = np.array([[0, 5, 1, 2], [3, 4, -1, -1]])
+    far = np.where(table < 0, -1, table + 140000 - 6)
+    g = torch.Generator(device="cuda").manual_seed(5)
+    T = sum(lens)
+    k, v = (torch.randn(T, Hkv, D, generator=g, device="cuda").bfloat16() for _ in range(2))
+    q = torch.randn(sum(tokens), 2 * Hkv, D, generator=g, device="cuda").bfloat16()
+    got = []
+    for cache, t in ((small, table), (large, far)):
+        slots = i32(np.concatenate([ref.slots_of(t[s], n, P) for s, n in enumerate(lens)]))
+        uc.uc_page_append(cache, k, v, slots)
+        ko, vo = torch.empty_like(k), torch.empty_like(v)
+        uc.uc_page_read(cache, slots, ko, vo)
+        out = [ko, vo]
+        for path in (uc.UC_PATH_AUTO, uc.UC_PATH_VALU):
+            o, lse = torch.empty_like(q), torch.empty(q.shape[:2], device="cuda")
+            prev = uc.uc_set_path(path)
+            try:
+                uc.uc_page_attend(cache, q, i32([0, 70, 71]), i32(lens), i32(t), 70, 0.09, o, lse)
+            finally:
+                uc.uc_set_path(prev)
+            out += [o, lse]
+        # a page's rows to another page
+        copies = i32([[t[0, 0], t[1, 0], 33]])
+        none = torch.empty(0, dtype=torch.int32, device="cuda")
+        uc.uc_page_append(cache, k[:0], v[:0], none, copies)
+        uc.uc_page_read(cache, slots, ko2 := torch.empty_like(k), vo2 := torch.empty_like(v))
+        got.append(out + [ko2, vo2])
+    for a, b in zip(*got):
+        assert torch.equal(a, b)
+    assert torch.equal(got[1][-1][200:233], got[1][1][:33])
+
+
+def paged_step(seed):
+    """A cache with a prompt among single tokens, and a call over it."""
+    lens, tokens = [300, 40, 555], [60, 1, 2]
+    cache, table = make_cache(lens, 32, 2, 128, 64, seed)
+    q = torch.tensor(np.random.default_rng(seed).standard_normal((63, 6, 128)), device="cuda").bfloat16()
+    dev, start, n, t = cache.device(uc), i32([0, 60, 61, 63]), i32(lens), i32(table)
+    ws = torch.empty(uc.uc_page_attend_workspace_size(dev, 6, 63, 3, 60), dtype=torch.uint8, device="cuda")
+
+    def run(o, lse, ws=ws, stream=None):
+        uc.uc_page_attend(dev, q, start, n, t, 60, 0.1, o, lse, ws, stream)
+    return run, q, ws
+
+
+def test_attention_on_another_stream():
+    run, q, _ = paged_step(91)
+    o, lse = torch.empty_like(q), torch.empty(63, 6, device="cuda")
+    run(o, lse)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    for given in (False, True):
+        o2, lse2 = torch.zeros_like(q), torch.zeros(63, 6, device="cuda")
+        s.wait_stream(torch.cuda.current_stream())
+        if given:
+            run(o2, lse2, stream=s)
+        else:
+            with torch.cuda.stream(s):
+                run(o2, lse2)
+        torch.cuda.current_stream().wait_stream(s)
+        assert torch.equal(o, o2) and torch.equal(lse, lse2)
+
+
+def test_two_graphs_share_a_workspace():
+    """Replayed in turn on one stream, with other work between."""
+    calls = [paged_step(92), paged_step(93)]
+    ws = calls[0][2]
+    want, graphs, outs = [], [], []
+    for run, q, _ in calls:
+        o, lse = torch.empty_like(q), torch.empty(63, 6, device="cuda")
+        run(o, lse, ws)
+        torch.cuda.synchronize()
+        want.append((o, lse))
+    for run, q, _ in calls:
+        o, lse = torch.empty_like(q), torch.empty(63, 6, device="cuda")
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            run(o, lse, ws)
+        graphs.append(graph)
+        outs.append((o, lse))
+    for _ in range(3):
+        for graph, (o, lse), (wo, wl) in zip(graphs, outs, want):
+            o.fill_(7.0)
+            lse.fill_(7.0)
+            ws.fill_(255)
+            graph.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(o, wo) and torch.equal(lse, wl)
+
+
+def test_results_repeat():
+    """Whatever the order its workgroups run in, a call gives the same bits."""
+    run, q, _ = paged_step(94)
+    outs = []
+    for _ in range(5):
+        o, lse = torch.empty_like(q), torch.empty(63, 6, device="cuda")
+        run(o, lse)
+        outs.append((o, lse))
+    assert all(torch.equal(o, outs[0][0]) and torch.equal(lse, outs[0][1]) for o, lse in outs)
+
+
 # ---------------------------------------------------------------- together
 
 def test_beam_search_over_the_cache():
