@@ -20,9 +20,10 @@
 //
 // Work is cut evenly without the host knowing any length: the tiles (64 keys)
 // of all sequences form one line, and workgroup w of W takes the w-th of W
-// equal pieces.  A sequence that lies within one piece is written by its
-// workgroup; one cut into several leaves a record (m, l, o) per piece, merged
-// by a second kernel in the order of the pieces.
+// equal pieces (or each of its waves one of 4 W, where sequences are many).  A
+// sequence that lies within one piece is written from there; one cut into
+// several leaves a record (m, l, o) per piece, merged by a second kernel in the
+// order of the pieces.
 #include <algorithm>
 
 #include "page_common.h"
@@ -183,11 +184,13 @@ struct Line {
 };
 
 // units of a sequence in the single-token kernel: its tiles, at least one so
-// that a row that sees nothing is written too, behind kStart units that stand
-// for what a sequence costs beside them; none where the prompt kernel takes it
+// that a row that sees nothing is written too, behind `start` units that stand
+// for what a sequence costs beside them (kStart; kSoloStart where a wave takes
+// it by itself); none where the prompt kernel takes it
+constexpr int kSoloStart = 2;
 __device__ inline int tiles_of(int rows) { return rows <= KT ? 1 : (int)(((uint32_t)rows + KT - 1) / KT); }
-__device__ inline int token_units(const Seq& x, int G) {
-  return x.n == 0 || (int64_t)x.n * G > 16 ? 0 : kStart + tiles_of(x.len);
+__device__ inline int token_units(const Seq& x, int G, int start) {
+  return x.n == 0 || (int64_t)x.n * G > 16 ? 0 : start + tiles_of(x.len);
 }
 
 // a sequence cut into pieces first .. last; rows of the call it stands for
@@ -303,33 +306,36 @@ __device__ inline float scaled_less(float x, float scale, float m) {
   return y - m;
 }
 
-// D, NG: head dim and groups of a row; QP: bf16 parts of a query element.
+// D, NG: head dim and groups of a row; QP: bf16 parts of a query element;
+// SOLO: a piece is a wave's, not the workgroup's.
 //
 // A wave's tile is four blocks of 16 keys, each within one page (pages are 16
 // rows or more), so a block's codes are one contiguous piece of the cache
 // behind a scalar address.  Block b's product rows are its keys, and lane
 // group g4 holds those of keys 16 b + 4 g4 + j; the transposing reads of the
 // values take their rows in that order.
-template <int D, int NG, int QP>
+template <int D, int NG, int QP, bool SOLO>
 __global__ __launch_bounds__(256, 2) void page_tokens_kernel(PageAttendArgs a, int W_all, float* __restrict__ rec,
                                                              Cut* __restrict__ cuts, int* __restrict__ units_out) {
   constexpr int KS = D / 32;  // matrix steps over the channels, words of a lane's codes of a row
   constexpr int DT = D / 16;  // tiles of 16 output channels
   constexpr int GS = KS / NG;
   constexpr int QT = QP == 1 ? UC_BF16 : UC_F16;
+  constexpr int STEP = SOLO ? 1 : WAVES, START = SOLO ? kSoloStart : kStart;
   using Lds = WaveLds<D, NG>;
   constexpr size_t kTiles = sizeof(Lds) * WAVES, kMerge = sizeof(float) * WAVES * 16 * (D + 2);
   __shared__ __attribute__((aligned(16))) char lds[kTiles > kMerge ? kTiles : kMerge];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int i16 = lane & 15, g4 = lane >> 4;
-  const int Hkv = a.pc.Hkv, h = blockIdx.x % Hkv, w = blockIdx.x / Hkv;
+  const int Hkv = a.pc.Hkv, h = blockIdx.x % Hkv, w = blockIdx.x / Hkv * (SOLO ? WAVES : 1) + (SOLO ? wave : 0);
   const int G = a.G, Hq = G * Hkv, lgP = a.pc.lgP, P1 = (1 << lgP) - 1;
   const Magic magic;
-  if (w == W_all) {  // one workgroup more where prompts follow: their plan
+  if ((int)(blockIdx.x / Hkv * (SOLO ? WAVES : 1)) == W_all) {  // one workgroup more where prompts follow: their plan
     plan_prompts(a, units_out, reinterpret_cast<int*>(lds));
     return;
   }
-  if (threadIdx.x == 0) cuts[blockIdx.x] = Cut{-1, 0, 0, 0};
+  const int turn = SOLO ? 0 : wave;  // the wave's among a piece's tiles
+  if (SOLO ? lane == 0 : threadIdx.x == 0) cuts[w * Hkv + h] = Cut{-1, 0, 0, 0};
 
   // this piece of the line; lane i counts sequences i c .. i c + c - 1
   const int c = (a.S + 63) / 64;
@@ -337,7 +343,7 @@ __global__ __launch_bounds__(256, 2) void page_tokens_kernel(PageAttendArgs a, i
   int mine = 0;
   for (int s = lane * c; s < min(a.S, (lane + 1) * c); ++s) {
     x = seq_of(a, s);
-    mine += token_units(x, G);
+    mine += token_units(x, G, START);
   }
   int upto = mine;
 #pragma unroll
@@ -348,7 +354,7 @@ __global__ __launch_bounds__(256, 2) void page_tokens_kernel(PageAttendArgs a, i
   const int U = __builtin_amdgcn_readlane(upto, 63);
   if (U == 0) return;
   // a sequence and a tile per wave at least
-  const Line line(U, max(1, min(W_all, U / (kStart + WAVES))));
+  const Line line(U, max(1, min(W_all, U / (START + STEP))));
   if (w >= line.W) return;
   const int u0 = line.first(w), u1 = line.first(w + 1);
   const int bucket = __builtin_ctzll(__builtin_amdgcn_ballot_w64(upto > u0));
@@ -394,19 +400,19 @@ __global__ __launch_bounds__(256, 2) void page_tokens_kernel(PageAttendArgs a, i
   // is none.  Its pages and queries are asked for.
   auto open = [&](int u) {
     for (;;) {
-      units = token_units(x, G);
+      units = token_units(x, G, START);
       if (before + units > u) break;
       before += units;
       if (before >= u1 || s + 1 >= a.S) return false;
       x = seq_of(a, ++s);
     }
-    if (before + kStart >= u1) return false;
-    t0 = max(0, u - before - kStart);
-    t1 = min(units, u1 - before) - kStart;
+    if (before + START >= u1) return false;
+    t0 = max(0, u - before - START);
+    t1 = min(units, u1 - before) - START;
     trow = a.table + (int64_t)s * a.ld;
     last16 = (x.len - 1) & ~15;  // first row of the last 16
-    page = page_for(t0 + wave);
-    page_next = page_for(t0 + wave + WAVES);
+    page = page_for(t0 + turn);
+    page_next = page_for(t0 + turn + STEP);
     const int r = min(i16, x.n * G - 1);
     const uint16_t* q = static_cast<const uint16_t*>(a.q) + (int64_t)(x.q0 + r / G) * a.q_ld +
                         (int64_t)(h * G + r % G) * D + g4 * 8;
@@ -417,9 +423,9 @@ __global__ __launch_bounds__(256, 2) void page_tokens_kernel(PageAttendArgs a, i
   // its first tile's loads
   auto first = [&]() {
     bad = false;
-    if (x.len > 0 && t0 + wave < t1) {
-      issue_values(t0 + wave, page);
-      issue_keys(t0 + wave, page);
+    if (x.len > 0 && t0 + turn < t1) {
+      issue_values(t0 + turn, page);
+      issue_keys(t0 + turn, page);
     }
   };
   if (!open(u0)) return;
@@ -470,9 +476,9 @@ __global__ __launch_bounds__(256, 2) void page_tokens_kernel(PageAttendArgs a, i
     for (int d = 0; d < DT; ++d) acc[d] = f4{0.f, 0.f, 0.f, 0.f};
 
     if (x.len > 0) {
-      int t = t0 + wave;
-      for (; t < t1; t += WAVES) {
-        const int tn = t + WAVES;
+      int t = t0 + turn;
+      for (; t < t1; t += STEP) {
+        const int tn = t + STEP;
         const bool more = tn < t1;
         // stage the tile: values as codes, words as floats; rows behind the
         // sequence hold anything, so their words become zeros
@@ -501,7 +507,7 @@ __global__ __launch_bounds__(256, 2) void page_tokens_kernel(PageAttendArgs a, i
         const int page_now = page_next;
         if (more) {
           issue_values(tn, page_now);
-          page_next = page_for(tn + WAVES);
+          page_next = page_for(tn + STEP);
         }
 
         // logits: p[4 b + j] of key 16 b + 4 g4 + j
@@ -602,7 +608,7 @@ __global__ __launch_bounds__(256, 2) void page_tokens_kernel(PageAttendArgs a, i
 
     // the next sequence's loads are under way while this one's waves merge
     const Seq now = x;
-    const int s_now = s, from = before + kStart, to = before + units;  // its tiles' units
+    const int s_now = s, from = before + START, to = before + units;  // its tiles' units
     bool more = to < u1 && s + 1 < a.S;
     const bool any = bad;
     if (more) {
@@ -616,6 +622,39 @@ __global__ __launch_bounds__(256, 2) void page_tokens_kernel(PageAttendArgs a, i
     for (int g = 0; g < NG; ++g) {
       low[g] += __shfl_xor(low[g], 16, 64);
       low[g] += __shfl_xor(low[g], 32, 64);
+    }
+    const bool begins = from >= u0, ends = to <= u1;
+    float* out = record<D, 16>(rec, w, Hkv, h, begins);
+    if (begins && !ends && (SOLO ? lane == 0 : threadIdx.x == 0))
+      cuts[w * Hkv + h] = Cut{s_now, w, line.piece_of(to - 1), 0};
+    if constexpr (SOLO) {
+      if (more) first();
+      if (__builtin_amdgcn_ballot_w64(any)) l = __builtin_nanf("");
+      if (i16 < nq) {
+        const int64_t at = (int64_t)(now.q0 + i16 / G) * Hq + h * G + i16 % G;
+        const bool whole = begins && ends;
+        const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+#pragma unroll
+        for (int d = 0; d < DT; ++d) {
+          f4 y = acc[d];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) y[j] += low[d / (DT / NG)];
+          if (whole) {
+            y *= inv;
+            const uint2 z =
+                QT == UC_BF16 ? uint2{bf2(y[0], y[1]), bf2(y[2], y[3])} : uint2{h2(y[0], y[1]), h2(y[2], y[3])};
+            *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.o) + at * D + d * 16 + g4 * 4) = z;
+          } else {
+            *reinterpret_cast<f4*>(out + i16 * kRec<D> + d * 16 + g4 * 4) = y;
+          }
+        }
+        if (g4 == 0) {
+          if (!whole) out[i16 * kRec<D> + D] = m, out[i16 * kRec<D> + D + 1] = l;
+          else if (a.lse) a.lse[at] = lse_of(m, l);
+        }
+      }
+      if (!more) break;
+      continue;
     }
     const int any_bad = __syncthreads_or(any);
     float* mo = reinterpret_cast<float*>(lds);  // [WAVES][16][D]
@@ -633,8 +672,6 @@ __global__ __launch_bounds__(256, 2) void page_tokens_kernel(PageAttendArgs a, i
     }
     if (more) first();
     __syncthreads();
-    const bool begins = from >= u0, ends = to <= u1;
-    float* out = record<D, 16>(rec, w, Hkv, h, begins);
     for (int e = threadIdx.x; e < nq * D; e += blockDim.x) {
       const int r = e / D, d = e % D;
       float M = kNone, ls = 0.0f, y = 0.0f;
@@ -659,7 +696,6 @@ __global__ __launch_bounds__(256, 2) void page_tokens_kernel(PageAttendArgs a, i
         }
       }
     }
-    if (begins && !ends && threadIdx.x == 0) cuts[blockIdx.x] = Cut{s_now, w, line.piece_of(to - 1), 0};
     if (!more) break;
     __syncthreads();  // LDS is written again
   }
@@ -1228,30 +1264,32 @@ __device__ inline void attend_block(const PageAttendArgs& a, RowLds<D>& lds, int
     attend_row<D, QT>(a, lds, x, s, x.q0 + r / a.G, h * a.G + r % a.G);
 }
 
-// Cuts of the token kernel (blocks [0, n_tokens) of the grid) and of the prompt
-// kernel (those behind).  Blocks that a piece marked as wide has a part in are
-// computed anew, whole ones of the piece by its own workgroups.
+// Two workgroups a cut of the token kernel (blocks [0, 2 n_tokens) of the
+// grid), sixteen a cut of the prompt kernel (those behind).  Blocks that a
+// piece marked as wide has a part in are computed anew, whole ones of the piece
+// by its own workgroups.
+constexpr int kMergeT = 2, kMergeP = 16;
 template <int D, int QT>
 __global__ __launch_bounds__(256, 8) void page_merge_kernel(PageAttendArgs a, int n_tokens, const Cut* __restrict__ cuts_t,
                                                          const float* __restrict__ rec_t,
                                                          const Cut* __restrict__ cuts_p,
                                                          const float* __restrict__ rec_p, int Wp,
                                                          const int* __restrict__ units, const int* __restrict__ wide) {
-  if ((int)blockIdx.x < n_tokens) {
-    if (blockIdx.y >= 2) return;
-    const Cut k = cuts_t[blockIdx.x];
-    if (k.seq >= 0) merge_cut<D, 16, QT>(a, k, blockIdx.x % a.pc.Hkv, rec_t, blockIdx.y, min((int)gridDim.y, 2));
+  if ((int)blockIdx.x < n_tokens * kMergeT) {
+    const int i = blockIdx.x / kMergeT;
+    const Cut k = cuts_t[i];
+    if (k.seq >= 0) merge_cut<D, 16, QT>(a, k, i % a.pc.Hkv, rec_t, blockIdx.x % kMergeT, kMergeT);
     return;
   }
   __shared__ RowLds<D> lds;
-  const int i = blockIdx.x - n_tokens, Hkv = a.pc.Hkv, h = i % Hkv, w = i / Hkv;
+  const int at = blockIdx.x - n_tokens * kMergeT, i = at / kMergeP, y = at % kMergeP, Hkv = a.pc.Hkv, h = i % Hkv, w = i / Hkv;
   const Cut k = cuts_p[i];
   const int all = wide[i];
   if (k.seq >= 0) {
     int any = 0;
     for (int j = k.first + threadIdx.x; j <= k.last; j += blockDim.x) any |= wide[j * Hkv + h];
-    if (__syncthreads_or(any)) attend_block<D, QT>(a, lds, k.seq, k.block, h, blockIdx.y, gridDim.y);
-    else merge_cut<D, QROWS, QT>(a, k, h, rec_p, blockIdx.y, gridDim.y);
+    if (__syncthreads_or(any)) attend_block<D, QT>(a, lds, k.seq, k.block, h, y, kMergeP);
+    else merge_cut<D, QROWS, QT>(a, k, h, rec_p, y, kMergeP);
   }
   if (!all) return;
   const int U = units[a.S];
@@ -1263,7 +1301,7 @@ __global__ __launch_bounds__(256, 8) void page_merge_kernel(PageAttendArgs a, in
     int before = units[s];
     for (int b = 0; b < prompt_blocks(x, a.G) && before < u1; ++b) {
       const int tiles = prompt_tiles(x, a.G, b);
-      if (before >= u0 && before + tiles <= u1) attend_block<D, QT>(a, lds, s, b * QROWS, h, blockIdx.y, gridDim.y);
+      if (before >= u0 && before + tiles <= u1) attend_block<D, QT>(a, lds, s, b * QROWS, h, y, kMergeP);
       before += tiles;
     }
   }
@@ -1271,10 +1309,19 @@ __global__ __launch_bounds__(256, 8) void page_merge_kernel(PageAttendArgs a, in
 
 }  // namespace
 
-// Pieces of the line per KV head: two workgroups per CU in one round for
-// single tokens, one (of twice the waves) for prompts.
-static int token_pieces(const PageCache& pc) { return std::max(1, 2 * device_cus() / pc.Hkv); }
+// Pieces of the line per KV head, each a workgroup's: for single tokens two
+// workgroups per CU in one round, for prompts one (of twice the waves).  Where
+// the sequences are many, each of a single-token workgroup's waves has a piece:
+// then waves neither idle on sequences of fewer tiles than there are waves, nor
+// meet at the end of every sequence.  1024 sequences of 128 rows take 34 us
+// that way and 75 the other, 256 of 64 rows 12 and 21, 512 of 2048 rows 120 and
+// 136; but 128 of 1024 rows 30 and 25, and one of 65536 rows 131 and 124 (more
+// records to merge).
 static int prompt_pieces(const PageCache& pc) { return std::max(1, device_cus() / pc.Hkv); }
+static bool solo_waves(const PageCache& pc, int S) { return S >= 2 * std::max(1, 2 * device_cus() / pc.Hkv); }
+static int token_pieces(const PageCache& pc, int S) {
+  return std::max(1, 2 * device_cus() / pc.Hkv) * (solo_waves(pc, S) ? WAVES : 1);
+}
 
 static size_t align_up(size_t x) { return (x + 255) & ~(size_t)255; }
 
@@ -1283,7 +1330,7 @@ static size_t align_up(size_t x) { return (x + 255) & ~(size_t)255; }
 struct PageWorkspace {
   size_t cuts_p, wide, units, rec_t, rec_p, end;
   PageWorkspace(const PageCache& pc, int S, bool prompts) {
-    const size_t nt = (size_t)token_pieces(pc) * pc.Hkv, np = (size_t)prompt_pieces(pc) * pc.Hkv;
+    const size_t nt = (size_t)token_pieces(pc, S) * pc.Hkv, np = (size_t)prompt_pieces(pc) * pc.Hkv;
     cuts_p = align_up(nt * sizeof(Cut));
     wide = cuts_p + (prompts ? align_up(np * sizeof(Cut)) : 0);
     units = wide + (prompts ? align_up(np * sizeof(int)) : 0);
@@ -1301,7 +1348,7 @@ size_t page_attend_workspace(const PageCache& pc, int G, int S, int max_q) {
 template <int D, int NG, int QP>
 static void launch_matrix(const PageAttendArgs& a, int max_q, void* ws, hipStream_t st) {
   constexpr int QT = QP == 1 ? UC_BF16 : UC_F16;
-  const bool prompts = (int64_t)max_q * a.G > 16;
+  const bool prompts = (int64_t)max_q * a.G > 16, solo = solo_waves(a.pc, a.S);
   const PageWorkspace at(a.pc, a.S, prompts);
   char* p = (char*)ws;
   Cut *cuts_t = (Cut*)p, *cuts_p = (Cut*)(p + at.cuts_p);
@@ -1309,16 +1356,20 @@ static void launch_matrix(const PageAttendArgs& a, int max_q, void* ws, hipStrea
   float *rec_t = (float*)(p + at.rec_t), *rec_p = (float*)(p + at.rec_p);
   // no more pieces than there can be work for
   const int64_t most = a.S * (kStart + std::max<int64_t>(1, (((int64_t)a.ld << a.pc.lgP) + KT - 1) / KT));
-  const int Wt = (int)std::max<int64_t>(1, std::min<int64_t>(token_pieces(a.pc), most / (kStart + WAVES)));
+  const int Wt = solo ? token_pieces(a.pc, a.S)
+                      : (int)std::max<int64_t>(1, std::min<int64_t>(token_pieces(a.pc, a.S), most / (kStart + WAVES)));
   const int nt = Wt * a.pc.Hkv, Wp = prompt_pieces(a.pc), np = prompts ? Wp * a.pc.Hkv : 0;
-  hipLaunchKernelGGL((page_tokens_kernel<D, NG, QP>), dim3(nt + (prompts ? 1 : 0)), dim3(256), 0, st, a, Wt, rec_t,
-                     cuts_t, units);
+  const dim3 grid((solo ? nt / WAVES : nt) + (prompts ? 1 : 0));
+  if (solo)
+    hipLaunchKernelGGL((page_tokens_kernel<D, NG, QP, true>), grid, dim3(256), 0, st, a, Wt, rec_t, cuts_t, units);
+  else
+    hipLaunchKernelGGL((page_tokens_kernel<D, NG, QP, false>), grid, dim3(256), 0, st, a, Wt, rec_t, cuts_t, units);
   if (prompts)
     hipLaunchKernelGGL((page_prompt_kernel<D, NG>), dim3(np), dim3(64 * PWAVES), 0, st, a, Wp, QP == 2, units, rec_p,
                        cuts_p, wide);
-  const int merge_t = Wt > 1 ? nt : 0, merge_p = np;
-  if (merge_t + merge_p)
-    hipLaunchKernelGGL((page_merge_kernel<D, QT>), dim3(merge_t + merge_p, merge_p ? 16 : 2), dim3(256), 0, st, a,
+  const int merge_t = Wt > 1 ? nt : 0;
+  if (merge_t + np)
+    hipLaunchKernelGGL((page_merge_kernel<D, QT>), dim3(merge_t * kMergeT + np * kMergeP), dim3(256), 0, st, a,
                        merge_t, cuts_t, rec_t, cuts_p, rec_p, Wp, units, wide);
 }
 

@@ -291,6 +291,33 @@ def test_many_sequences(tokens):
     check(*run_attend(cache, table, lens, toks, 4, "bf16", 5), "bf16")
 
 
+@pytest.mark.parametrize("dtype,D,group,tokens", [("bf16", 128, 64, 1), ("f16", 128, 32, 40), ("bf16", 64, 32, 3)])
+def test_a_piece_of_the_line_for_every_wave(dtype, D, group, tokens):
+    """Many short sequences, three of them long enough to be cut, one with a
+    page outside the cache, some without tokens or rows."""
+    r = np.random.default_rng(71)
+    S, Hkv, P = 300, 4, 16
+    lens = [int(x) for x in r.integers(0, 150, S)]
+    toks = [int(x) for x in r.integers(0, 3, S)]
+    for s, n in ((0, 900), (150, 2600), (299, 1100)):
+        lens[s], toks[s] = n, 2
+    lens[200], toks[200] = 170, tokens
+    lens[77], toks[77] = 60, 2
+    cache, table = make_cache(lens, P, Hkv, D, group, 72)
+    good = np.array(table)
+    table[77, 1] = cache.n_pages
+    start = np.concatenate([[0], np.cumsum(toks)])
+    T = int(start[-1])
+    q = torch.tensor(r.standard_normal((T, 2 * Hkv, D)), device="cuda").to(DT[dtype])
+    o, lse = torch.empty_like(q), torch.empty(T, 2 * Hkv, device="cuda")
+    uc.uc_page_attend(cache.device(uc), q, i32(start), i32(lens), i32(table), max(toks), 0.1, o, lse)
+    want, want_lse = ref.attend(cache, f64(q), start, lens, good, float(np.float32(0.1)))
+    a, b = int(start[77]), int(start[78])
+    assert torch.isnan(o[a:b]).all() and torch.isnan(lse[a:b]).all()
+    keep = np.r_[0:a, b:T]
+    check(o[keep], lse[keep], want[keep], want_lse[keep], dtype)
+
+
 @pytest.mark.parametrize("tokens", [1, 20])
 def test_sharp_logits(tokens):
     """Logits far apart: one key takes all, references rise step by step."""
