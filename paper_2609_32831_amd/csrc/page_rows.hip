@@ -68,6 +68,9 @@ struct RowArgs {
   int n_copies;
 };
 
+// a quotient to its code, nearest even
+__device__ inline uint32_t code_of(float q) { return (uint32_t)__builtin_amdgcn_fmed3f(rintf(q), 0.0f, 15.0f); }
+
 // blocks [0, row_blocks): rows; then one block per copy.
 template <int D, int DT>
 __global__ __launch_bounds__(256) void page_append_kernel(RowArgs a, int row_blocks) {
@@ -111,11 +114,22 @@ __global__ __launch_bounds__(256) void page_append_kernel(RowArgs a, int row_blo
   const float m = bf16_to_f32(mb);
   const uint32_t sb = (__float_as_uint(fmaxf(hi - m, 0.0f) / 15.0f) + 0x000FFFFFu) & 0xFFF00000u;
   const float s = __uint_as_float(sb);
+  // Quotients rounded as IEEE division does, by one reciprocal for all: with
+  // r = 1 / s rounded to nearest and q within an ulp of d / s, q + (d - q s) r
+  // is d / s rounded to nearest (Markstein 1990, for a divisor whose bits are
+  // not all ones; s has four).  In this range of s nothing that counts passes
+  // the type's range.
   uint32_t w = 0;
+  if (s >= 0x1p-90f && s <= 0x1p100f) {
+    const float r = 1.0f / s;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    const float q = s > 0.0f ? fminf(fmaxf(rintf((x[e] - m) / s), 0.0f), 15.0f) : 0.0f;
-    w |= (uint32_t)q << (4 * e);
+    for (int e = 0; e < 8; ++e) {
+      const float d = x[e] - m, q = d * r;
+      w |= code_of(fmaf(fmaf(-q, s, d), r, q)) << (4 * e);
+    }
+  } else if (s > 0.0f) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) w |= code_of((x[e] - m) / s) << (4 * e);
   }
   const int64_t row = page_row(slot >> pc.lgP, pc.Hkv, h, pc.lgP, slot);
   uint32_t* codes = (uint32_t*)(values ? pc.codes_v : pc.codes_k);

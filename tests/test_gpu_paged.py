@@ -122,6 +122,32 @@ def test_rows_of_special_values():
     assert np.all(np.isfinite(host.rows(range(8))[0]))  # what a mask hides cannot spread
 
 
+@pytest.mark.parametrize("group", [32, 64, 128])
+def test_codes_of_rows_of_many_sizes(group):
+    """Codes are those of IEEE division whatever the step: rows of every size,
+    and quotients on and next to the halves that rounding parts at."""
+    r = np.random.default_rng(group)
+    D, P, T = 128, 64, 1024
+    x = r.standard_normal((T, 2, D)) * 2.0 ** r.integers(-124, 124, (T, 2, 1))
+    for t in range(256):  # a minimum and a maximum that give the step s, the rest near (k + 1/2) s
+        s = 2.0 ** r.integers(-20, 20) * r.integers(8, 16) / 8
+        m = s * r.integers(-30, 3)
+        y = (m + (r.integers(0, 15, (2, D)) + 0.5) * s).astype(np.float32)
+        for _ in range(2):
+            y = np.where(r.random(y.shape) < 0.5, np.nextafter(y, np.float32(r.choice([-np.inf, np.inf]))), y)
+        y[:, ::32], y[:, 1::32] = m, m + 15 * s
+        x[t] = y
+    x = np.clip(x, -3e38, 3e38).astype(np.float32)
+    host = ref.Cache(T // P, P, 2, D, group, 5)
+    cache = host.device(uc)
+    t = torch.from_numpy(x).cuda()
+    uc.uc_page_append(cache, t, t, i32(range(T)))
+    with np.errstate(over="ignore"):
+        host.append(x, x, range(T))
+    for name, want in (("codes_k", host.ck), ("codes_v", host.cv), ("scale_k", host.sk), ("scale_v", host.sv)):
+        assert np.array_equal(cache.t[name].cpu().numpy().view(np.uint8), want.view(np.uint8)), name
+
+
 def test_copies_join_the_append():
     D, group, P, Hkv = 64, 32, 16, 2
     host = ref.Cache(6, P, Hkv, D, group, 5)
