@@ -77,65 +77,75 @@ __global__ __launch_bounds__(256) void page_append_kernel(RowArgs a, int row_blo
   constexpr int LANES = D / 8;
   const PageCache& pc = a.cache;
   const int P = 1 << pc.lgP, ng = pc.ng;
+  const int h = blockIdx.y;
   if ((int)blockIdx.x >= row_blocks) {
     // rows 0 .. n-1 of every head of a page, to another page
     const int32_t* cp = a.copies + 3 * ((int)blockIdx.x - row_blocks);
     const int src = cp[0], dst = cp[1], n = min(cp[2], P);
     if ((uint32_t)src >= (uint32_t)pc.n_pages || (uint32_t)dst >= (uint32_t)pc.n_pages || src == dst || n <= 0) return;
-    const int h = blockIdx.y >> 1;
     const int64_t from = page_row(src, pc.Hkv, h, pc.lgP, 0), to = page_row(dst, pc.Hkv, h, pc.lgP, 0);
-    uint32_t* codes = (uint32_t*)(blockIdx.y & 1 ? pc.codes_v : pc.codes_k);
-    uint32_t* scale = (uint32_t*)(blockIdx.y & 1 ? pc.scale_v : pc.scale_k);
-    for (int i = threadIdx.x; i < n * (D / 8); i += blockDim.x) codes[to * (D / 8) + i] = codes[from * (D / 8) + i];
-    for (int i = threadIdx.x; i < n * ng; i += blockDim.x) scale[to * ng + i] = scale[from * ng + i];
+#pragma unroll
+    for (int kv = 0; kv < 2; ++kv) {
+      uint32_t* codes = (uint32_t*)(kv ? pc.codes_v : pc.codes_k);
+      uint32_t* scale = (uint32_t*)(kv ? pc.scale_v : pc.scale_k);
+      for (int i = threadIdx.x; i < n * (D / 8); i += blockDim.x) codes[to * (D / 8) + i] = codes[from * (D / 8) + i];
+      for (int i = threadIdx.x; i < n * ng; i += blockDim.x) scale[to * ng + i] = scale[from * ng + i];
+    }
     return;
   }
-  const int h = blockIdx.y >> 1;
-  const bool values = blockIdx.y & 1;
   const int t = blockIdx.x * (256 / LANES) + threadIdx.x / LANES, c = threadIdx.x % LANES;
-  const int slot = t < a.T ? a.slots[t] : -1;
+  // the row and its slot at a time, wherever it goes
+  float x[2][8] = {};
+  int slot = -1;
+  if (t < a.T) {
+    load8<DT>(a.k, (int64_t)t * a.ld + h * D + c * 8, x[0]);
+    load8<DT>(a.v, (int64_t)t * a.ld + h * D + c * 8, x[1]);
+    slot = a.slots[t];
+  }
   const bool live = slot >= 0 && (slot >> pc.lgP) < pc.n_pages;
-  float x[8] = {};
-  if (live) load8<DT>(values ? a.v : a.k, (int64_t)t * a.ld + h * D + c * 8, x);
-  float lo = INFINITY, hi = -INFINITY;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    x[e] = x[e] != x[e] ? 0.0f : fminf(fmaxf(x[e], -kMost), kMost);
-    lo = fminf(lo, x[e]);
-    hi = fmaxf(hi, x[e]);
-  }
+  const int64_t row = live ? page_row(slot >> pc.lgP, pc.Hkv, h, pc.lgP, slot) : 0;
   const int per = LANES / ng;  // lanes of one group
-  for (int o = 1; o < per; o <<= 1) {
-    lo = fminf(lo, __shfl_xor(lo, o, 64));
-    hi = fmaxf(hi, __shfl_xor(hi, o, 64));
-  }
-  if (!live) return;
-  const uint32_t mb = f32_to_bf16_bits(lo);
-  const float m = bf16_to_f32(mb);
-  const uint32_t sb = (__float_as_uint(fmaxf(hi - m, 0.0f) / 15.0f) + 0x000FFFFFu) & 0xFFF00000u;
-  const float s = __uint_as_float(sb);
-  // Quotients rounded as IEEE division does, by one reciprocal for all: with
-  // r = 1 / s rounded to nearest and q within an ulp of d / s, q + (d - q s) r
-  // is d / s rounded to nearest (Markstein 1990, for a divisor whose bits are
-  // not all ones; s has four).  In this range of s nothing that counts passes
-  // the type's range.
-  uint32_t w = 0;
-  if (s >= 0x1p-90f && s <= 0x1p100f) {
-    const float r = 1.0f / s;
+#pragma unroll
+  for (int kv = 0; kv < 2; ++kv) {
+    float(&y)[8] = x[kv];
+    float lo = INFINITY, hi = -INFINITY;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      const float d = x[e] - m, q = d * r;
-      w |= code_of(fmaf(fmaf(-q, s, d), r, q)) << (4 * e);
+      y[e] = y[e] != y[e] ? 0.0f : fminf(fmaxf(y[e], -kMost), kMost);
+      lo = fminf(lo, y[e]);
+      hi = fmaxf(hi, y[e]);
     }
-  } else if (s > 0.0f) {
+    for (int o = 1; o < per; o <<= 1) {
+      lo = fminf(lo, __shfl_xor(lo, o, 64));
+      hi = fmaxf(hi, __shfl_xor(hi, o, 64));
+    }
+    const uint32_t mb = f32_to_bf16_bits(lo);
+    const float m = bf16_to_f32(mb);
+    const uint32_t sb = (__float_as_uint(fmaxf(hi - m, 0.0f) / 15.0f) + 0x000FFFFFu) & 0xFFF00000u;
+    const float s = __uint_as_float(sb);
+    // Quotients rounded as IEEE division does, by one reciprocal for all: with
+    // r = 1 / s rounded to nearest and q within an ulp of d / s, q + (d - q s) r
+    // is d / s rounded to nearest (Markstein 1990, for a divisor whose bits are
+    // not all ones; s has four).  In this range of s nothing that counts passes
+    // the type's range.
+    uint32_t w = 0;
+    if (s >= 0x1p-90f && s <= 0x1p100f) {
+      const float r = 1.0f / s;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) w |= code_of((x[e] - m) / s) << (4 * e);
+      for (int e = 0; e < 8; ++e) {
+        const float d = y[e] - m, q = d * r;
+        w |= code_of(fmaf(fmaf(-q, s, d), r, q)) << (4 * e);
+      }
+    } else if (s > 0.0f) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) w |= code_of((y[e] - m) / s) << (4 * e);
+    }
+    if (!live) continue;
+    uint32_t* codes = (uint32_t*)(kv ? pc.codes_v : pc.codes_k);
+    uint32_t* scale = (uint32_t*)(kv ? pc.scale_v : pc.scale_k);
+    codes[row * (D / 8) + (kv ? code_word<D, false>(c) : code_word<D, true>(c))] = w;
+    if (c % per == 0) scale[row * ng + c / per] = (sb >> 16) | (mb << 16);
   }
-  const int64_t row = page_row(slot >> pc.lgP, pc.Hkv, h, pc.lgP, slot);
-  uint32_t* codes = (uint32_t*)(values ? pc.codes_v : pc.codes_k);
-  uint32_t* scale = (uint32_t*)(values ? pc.scale_v : pc.scale_k);
-  codes[row * (D / 8) + (values ? code_word<D, false>(c) : code_word<D, true>(c))] = w;
-  if (c % per == 0) scale[row * ng + c / per] = (sb >> 16) | (mb << 16);
 }
 
 template <int D, int DT>
@@ -166,7 +176,7 @@ hipError_t launch_page_append(const PageCache& pc, const void* k, const void* v,
   const int per = 256 / (pc.D / 8), row_blocks = (T + per - 1) / per;
   if (row_blocks + n_copies == 0) return hipSuccess;
   const RowArgs a{pc, k, v, ld, T, slots, copies, n_copies};
-  const dim3 grid(row_blocks + n_copies, 2 * pc.Hkv);
+  const dim3 grid(row_blocks + n_copies, pc.Hkv);
 #define UC_APPEND(DIM, TYPE) \
   hipLaunchKernelGGL((page_append_kernel<DIM, TYPE>), grid, dim3(256), 0, st, a, row_blocks)
   if (pc.D == 128) {
