@@ -661,14 +661,15 @@ uc_status uc_page_step(int S, int page_rows, int n_pages, const int32_t* len, co
  * passed over; no slot may occur twice.  copies, when n_copies > 0, is device
  * int32 [n_copies, 3] as uc_beam_reorder writes it: rows 0 .. rows - 1 of page
  * `from` are copied to page `to` (from < 0: nothing); the same call's slots
- * must not lie in rows that are copied.  T <= 2^27, n_copies <= 2^22. */
+ * must not lie in rows that are copied.  T * Hkv <= 2^27 and n_copies * Hkv
+ * <= 2^22. */
 uc_status uc_page_append(const uc_page_cache* cache, const void* k_new, const void* v_new,
                          uc_dtype dt, int64_t ld, int T, const int32_t* slots,
                          const int32_t* copies, int n_copies, void* stream);
 
 /* The values held in T slots, as dense rows: k_out and v_out at t * ld + h * D
  * in dt (alignment as for uc_page_append).  A slot outside the cache gives
- * zeros.  T <= 2^27. */
+ * zeros.  T * Hkv <= 2^27. */
 uc_status uc_page_read(const uc_page_cache* cache, const int32_t* slots, int T, void* k_out,
                        void* v_out, uc_dtype dt, int64_t ld, void* stream);
 

@@ -34,9 +34,9 @@ hipError_t launch_beam_reorder(const int32_t* parent, const int32_t* token, cons
 
 namespace {
 
-// rows of an append or a read: 16 or more to a workgroup of 256, of which a
-// launch holds fewer than 2^24
-constexpr int kMostRows = 1 << 27;
+// an append or a read: 16 heads' rows or more to a workgroup of 256, a page's
+// head to another; a launch holds fewer than 2^24 of them
+constexpr int64_t kMostRows = 1 << 27, kMostCopies = 1 << 22;
 
 bool aligned4(const void* p) { return ((uintptr_t)p & 3u) == 0; }
 
@@ -125,7 +125,8 @@ uc_status uc_page_append(const uc_page_cache* cache, const void* k_new, const vo
   uc_status st = check_cache(cache, pc);
   if (st) return st;
   if (T < 0 || n_copies < 0) return fail(UC_E_INVALID, "T and n_copies must be >= 0 (got %d, %d)", T, n_copies);
-  if (T > kMostRows || n_copies > kMostRows / 32) return fail(UC_E_UNSUPPORTED, "too many rows or copies for one call");
+  if ((int64_t)T * pc.Hkv > kMostRows || (int64_t)n_copies * pc.Hkv > kMostCopies)
+    return fail(UC_E_UNSUPPORTED, "too many rows or copies for one call");
   if (T > 0 && ((st = check_rows("k_new", k_new, dt, ld, (int64_t)pc.Hkv * pc.D)) ||
                 (st = check_rows("v_new", v_new, dt, ld, (int64_t)pc.Hkv * pc.D)) || (st = check_ints("slots", slots))))
     return st;
@@ -140,7 +141,7 @@ uc_status uc_page_read(const uc_page_cache* cache, const int32_t* slots, int T, 
   uc_status st = check_cache(cache, pc);
   if (st) return st;
   if (T < 0) return fail(UC_E_INVALID, "T must be >= 0 (got %d)", T);
-  if (T > kMostRows) return fail(UC_E_UNSUPPORTED, "too many rows for one call");
+  if ((int64_t)T * pc.Hkv > kMostRows) return fail(UC_E_UNSUPPORTED, "too many rows for one call");
   if (T == 0 && !dtype_ok(dt)) return fail(UC_E_INVALID, "bad dtype %d", dt);
   if (T > 0 && ((st = check_rows("k_out", k_out, dt, ld, (int64_t)pc.Hkv * pc.D)) ||
                 (st = check_rows("v_out", v_out, dt, ld, (int64_t)pc.Hkv * pc.D)) || (st = check_ints("slots", slots))))

@@ -66,10 +66,10 @@ CASES = [
      [(dict(S=0), E), (dict(ld=0), E), (dict(n_slots=-1), E), (dict(refused=None), E)]),
     ("uc_page_append", APPEND, rows("k", "v") + ints("slots", "copies") +
      [(dict(dt=7), E), (dict(dt=-1, T=0), E), (dict(ld=511), E), (dict(ld=516), E), (dict(T=-1), E),
-      (dict(n_copies=-1), E), (dict(T=(1 << 27) + 1), U), (dict(n_copies=(1 << 22) + 1), U)]),
+      (dict(n_copies=-1), E), (dict(T=(1 << 25) + 1), U), (dict(n_copies=(1 << 20) + 1), U)]),
     ("uc_page_read", READ, rows("k", "v") + ints("slots") +
      [(dict(dt=3), E), (dict(ld=504), E), (dict(ld=514, dt=uc.UC_F32), E), (dict(T=-1), E),
-      (dict(T=(1 << 27) + 1), U)]),
+      (dict(T=(1 << 25) + 1), U)]),
     ("uc_page_attend", ATTEND, rows("q", "o") + ints("q_start", "len", "table") +
      [(dict(Hq=0), E), (dict(Hq=30), E), (dict(dt=9), E), (dict(q_ld=28 * 128 - 8), E), (dict(q_ld=28 * 128 + 4), E),
       (dict(T=-1), E), (dict(S=0), E), (dict(max_q=0), E), (dict(ld=0), E), (dict(lse=FAKE + 2), E),
