@@ -689,7 +689,7 @@ uc_status uc_page_read(const uc_page_cache* cache, const int32_t* slots, int T, 
  * Tokens of no sequence keep their o and lse.  q_start and len are held to
  * [0, T] and the table's rows.  Rows of a sequence whose table names a page
  * outside the cache within its length may be NaN, and those that see it are.
- * Sequences with n * (Hq / Hkv) <= 16 and longer ones are taken by kernels of
+ * Sequences with n * (Hq / Hkv) <= 64 and longer ones are taken by kernels of
  * their own in the same call ("page_tokens", "page_prompt" for
  * uc_last_kernel; UC_F32 queries and UC_PATH_VALU: "page_valu").  ws:
  * uc_page_attend_workspace_size bytes; its size depends on the arguments

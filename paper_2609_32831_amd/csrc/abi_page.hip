@@ -167,10 +167,10 @@ uc_status uc_page_attend(const uc_page_cache* cache, int Hq, const void* q, uc_d
   if (!dtype_ok(q_dt)) return fail(UC_E_INVALID, "bad q dtype %d", q_dt);
   if (!(sm_scale > 0.0f) || !isfinite(sm_scale * kLog2e)) return fail(UC_E_INVALID, "sm_scale must be finite and > 0");
   if ((int64_t)T * Hq > INT32_MAX) return fail(UC_E_UNSUPPORTED, "too many query rows");
-  // units of work: tiles of 64 rows and what a sequence counts beside them,
-  // for every block of 256 query rows, taken as 128
+  // units of work: tiles of 64 rows and what a block counts beside them, for
+  // every block of few query rows and of 256, taken as 128
   const int64_t tiles = ((int64_t)table_ld * cache->page_rows + 63) / 64 + kStart;
-  if (tiles > INT32_MAX / 64 || tiles * ((int64_t)S + (int64_t)T * (Hq / pc.Hkv) / 128) > INT32_MAX)
+  if (tiles > INT32_MAX / 64 || tiles * ((int64_t)S * kFewBlocks + (int64_t)T * (Hq / pc.Hkv) / 128) > INT32_MAX)
     return fail(UC_E_UNSUPPORTED, "tables of %d pages for %d sequences and %d tokens hold too much work for one call",
                 table_ld, S, T);
   if ((st = check_ints("q_start", q_start)) || (st = check_ints("len", len)) || (st = check_ints("table", table)))

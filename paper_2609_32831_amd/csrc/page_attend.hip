@@ -1,5 +1,5 @@
 // page_attend.hip -- attention over a paged cache held in 4 bits: single
-// tokens (at most 16 query rows of a KV head), prompts (any number), and the
+// tokens (few query rows of a KV head), prompts (any number), and the
 // vector-ALU form that stands for both.
 //
 // A sequence of len rows whose last n are this call's queries: query i sees
@@ -183,17 +183,23 @@ struct Line {
   }
 };
 
-// units of a sequence in the single-token kernel: its tiles, at least one so
-// that a row that sees nothing is written too, behind `start` units that stand
-// for what a sequence costs beside them (kStart; kSoloStart where a wave takes
-// it by itself); none where the prompt kernel takes it
+// The single-token kernel takes the query rows of a KV head in blocks of 16, of
+// sequences with kFewBlocks of them at most; 0 where the prompt kernel takes
+// it, which works on 256 rows whatever their number (64 sequences of 4096 rows
+// with 21, 28, 42, 63 query rows for each of 4 heads: 69, 69, 104, 127 us here,
+// 199 to 204 there).
+__device__ inline int token_blocks(const Seq& x, int G) {
+  const int64_t rows = (int64_t)x.n * G;
+  return rows > 16 * kFewBlocks ? 0 : (int)(rows + 15) >> 4;
+}
+// units of a block: the sequence's tiles, at least one so that a row that sees
+// nothing is written too, behind `start` units that stand for what a block
+// costs beside them (kStart; kSoloStart where a wave takes it by itself)
 constexpr int kSoloStart = 2;
 __device__ inline int tiles_of(int rows) { return rows <= KT ? 1 : (int)(((uint32_t)rows + KT - 1) / KT); }
-__device__ inline int token_units(const Seq& x, int G, int start) {
-  return x.n == 0 || (int64_t)x.n * G > 16 ? 0 : start + tiles_of(x.len);
-}
 
-// a sequence cut into pieces first .. last; rows of the call it stands for
+// a block of a sequence (its first row among the sequence's) cut into pieces
+// first .. last
 struct Cut {
   int seq, first, last, block;
 };
@@ -214,7 +220,7 @@ constexpr int PWAVES = 8, QROWS = 32 * PWAVES;
 // blocks of a sequence
 __device__ inline int prompt_blocks(const Seq& x, int G) {
   const int64_t rows = (int64_t)x.n * G;
-  return rows <= 16 ? 0 : (int)((rows + QROWS - 1) / QROWS);
+  return rows <= 16 * kFewBlocks ? 0 : (int)((rows + QROWS - 1) / QROWS);
 }
 // tiles of its block b, at least one
 __device__ inline int prompt_tiles(const Seq& x, int G, int b) {
@@ -343,7 +349,7 @@ __global__ __launch_bounds__(256, 2) void page_tokens_kernel(PageAttendArgs a, i
   int mine = 0;
   for (int s = lane * c; s < min(a.S, (lane + 1) * c); ++s) {
     x = seq_of(a, s);
-    mine += token_units(x, G, START);
+    mine += token_blocks(x, G) * (START + tiles_of(x.len));
   }
   int upto = mine;
 #pragma unroll
@@ -367,8 +373,9 @@ __global__ __launch_bounds__(256, 2) void page_tokens_kernel(PageAttendArgs a, i
   }
   Lds& L = *reinterpret_cast<Lds*>(lds + wave * sizeof(Lds));
 
-  // The sequence at hand: tiles [t0, t1) of it lie in this piece.
-  int units = 0, t0 = 0, t1 = 0, page = 0, page_next = 0, last16 = 0;
+  // The block at hand, `blk` of the sequence's `blks`: tiles [t0, t1) of it lie
+  // in this piece.
+  int blk = 0, blks = 0, units = 0, t0 = 0, t1 = 0, page = 0, page_next = 0, last16 = 0;
   const int32_t* trow = nullptr;
   u4 raw[KS];                                    // the lane's query row
   uint32_t ck[4][KS], cv[4][KS], wk[NG], wv[NG];  // a tile
@@ -396,16 +403,21 @@ __global__ __launch_bounds__(256, 2) void page_tokens_kernel(PageAttendArgs a, i
     load_words<NG>(a.pc.scale_k + row * NG, wk);
     load_words<NG>(a.pc.scale_v + row * NG, wv);
   };
-  // on to the first sequence from s on with tiles in [u, u1); false if there
-  // is none.  Its pages and queries are asked for.
+  // on to the first block from this one on with tiles in [u, u1); false if
+  // there is none.  Its pages and queries are asked for.
   auto open = [&](int u) {
     for (;;) {
-      units = token_units(x, G, START);
-      if (before + units > u) break;
-      before += units;
+      blks = token_blocks(x, G);
+      units = START + tiles_of(x.len);
+      if (before + (blks - blk) * units > u) break;
+      before += (blks - blk) * units;
       if (before >= u1 || s + 1 >= a.S) return false;
       x = seq_of(a, ++s);
+      blk = 0;
     }
+    const int ahead = (u - before) / units;
+    blk += ahead;
+    before += ahead * units;
     if (before + START >= u1) return false;
     t0 = max(0, u - before - START);
     t1 = min(units, u1 - before) - START;
@@ -413,7 +425,7 @@ __global__ __launch_bounds__(256, 2) void page_tokens_kernel(PageAttendArgs a, i
     last16 = (x.len - 1) & ~15;  // first row of the last 16
     page = page_for(t0 + turn);
     page_next = page_for(t0 + turn + STEP);
-    const int r = min(i16, x.n * G - 1);
+    const int r = min(blk * 16 + i16, x.n * G - 1);
     const uint16_t* q = static_cast<const uint16_t*>(a.q) + (int64_t)(x.q0 + r / G) * a.q_ld +
                         (int64_t)(h * G + r % G) * D + g4 * 8;
 #pragma unroll
@@ -432,7 +444,7 @@ __global__ __launch_bounds__(256, 2) void page_tokens_kernel(PageAttendArgs a, i
   first();
 
   for (;;) {
-    const int nq = x.n * G;
+    const int nq = min(16, x.n * G - blk * 16);
     // queries: the operand's channel order pairs codes i and i + 4
     u4 qb[QP][KS];
     float sq[NG];  // sum of the group's channels, all of them in every lane
@@ -464,8 +476,8 @@ __global__ __launch_bounds__(256, 2) void page_tokens_kernel(PageAttendArgs a, i
       }
     }
     // first row that the lane's query does not see, and the least of them all
-    const int lim = max(0, min(x.len, (int)((int64_t)x.len - x.n + min(i16, nq - 1) / G + 1)));
-    const int lim_all = max(0, (int)((int64_t)x.len - x.n + 1));
+    const int lim = max(0, min(x.len, (int)((int64_t)x.len - x.n + (blk * 16 + min(i16, nq - 1)) / G + 1)));
+    const int lim_all = max(0, (int)min((int64_t)x.len, (int64_t)x.len - x.n + blk * 16 / G + 1));
 
     bool far = false;
     float m = kNone, l = 0.0f, low[NG];
@@ -606,14 +618,14 @@ __global__ __launch_bounds__(256, 2) void page_tokens_kernel(PageAttendArgs a, i
       }
     }
 
-    // the next sequence's loads are under way while this one's waves merge
+    // the next block's loads are under way while this one's waves merge
     const Seq now = x;
-    const int s_now = s, from = before + START, to = before + units;  // its tiles' units
-    bool more = to < u1 && s + 1 < a.S;
+    const int s_now = s, r_now = blk * 16, from = before + START, to = before + units;  // its tiles' units
+    bool more = to < u1;
     const bool any = bad;
     if (more) {
       before = to;
-      x = seq_of(a, ++s);
+      ++blk;
       more = open(to);
     }
     l += __shfl_xor(l, 16, 64);
@@ -626,12 +638,12 @@ __global__ __launch_bounds__(256, 2) void page_tokens_kernel(PageAttendArgs a, i
     const bool begins = from >= u0, ends = to <= u1;
     float* out = record<D, 16>(rec, w, Hkv, h, begins);
     if (begins && !ends && (SOLO ? lane == 0 : threadIdx.x == 0))
-      cuts[w * Hkv + h] = Cut{s_now, w, line.piece_of(to - 1), 0};
+      cuts[w * Hkv + h] = Cut{s_now, w, line.piece_of(to - 1), r_now};
     if constexpr (SOLO) {
       if (more) first();
       if (__builtin_amdgcn_ballot_w64(any)) l = __builtin_nanf("");
       if (i16 < nq) {
-        const int64_t at = (int64_t)(now.q0 + i16 / G) * Hq + h * G + i16 % G;
+        const int64_t at = (int64_t)(now.q0 + (r_now + i16) / G) * Hq + h * G + (r_now + i16) % G;
         const bool whole = begins && ends;
         const float inv = l == 0.0f ? 0.0f : 1.0f / l;
 #pragma unroll
@@ -685,7 +697,7 @@ __global__ __launch_bounds__(256, 2) void page_tokens_kernel(PageAttendArgs a, i
       }
       if (any_bad) ls = __builtin_nanf("");
       if (begins && ends) {
-        const int64_t at = (int64_t)(now.q0 + r / G) * Hq + h * G + r % G;
+        const int64_t at = (int64_t)(now.q0 + (r_now + r) / G) * Hq + h * G + (r_now + r) % G;
         put<QT>(a.o, at * D + d, ls == 0.0f ? 0.0f : y / ls);
         if (d == 0 && a.lse) a.lse[at] = lse_of(M, ls);
       } else {
@@ -1342,22 +1354,27 @@ struct PageWorkspace {
 };
 
 size_t page_attend_workspace(const PageCache& pc, int G, int S, int max_q) {
-  return PageWorkspace(pc, S, (int64_t)max_q * G > 16).end;
+  return PageWorkspace(pc, S, (int64_t)max_q * G > 16 * kFewBlocks).end;
 }
 
 template <int D, int NG, int QP>
 static void launch_matrix(const PageAttendArgs& a, int max_q, void* ws, hipStream_t st) {
   constexpr int QT = QP == 1 ? UC_BF16 : UC_F16;
-  const bool prompts = (int64_t)max_q * a.G > 16, solo = solo_waves(a.pc, a.S);
+  const bool prompts = (int64_t)max_q * a.G > 16 * kFewBlocks;
   const PageWorkspace at(a.pc, a.S, prompts);
   char* p = (char*)ws;
   Cut *cuts_t = (Cut*)p, *cuts_p = (Cut*)(p + at.cuts_p);
   int *units = (int*)(p + at.units), *wide = (int*)(p + at.wide);
   float *rec_t = (float*)(p + at.rec_t), *rec_p = (float*)(p + at.rec_p);
-  // no more pieces than there can be work for
-  const int64_t most = a.S * (kStart + std::max<int64_t>(1, (((int64_t)a.ld << a.pc.lgP) + KT - 1) / KT));
-  const int Wt = solo ? token_pieces(a.pc, a.S)
-                      : (int)std::max<int64_t>(1, std::min<int64_t>(token_pieces(a.pc, a.S), most / (kStart + WAVES)));
+  // The tiles there can be: where they are no more than the pieces, a wave takes
+  // each by itself as well (one sequence of 777 rows: 13.3 us, and 14.9 in one
+  // workgroup); and no more pieces than there can be work for.
+  const int64_t blocks = a.S * std::min<int64_t>(kFewBlocks, ((int64_t)max_q * a.G + 15) / 16);
+  const int64_t tiles = std::max<int64_t>(1, (((int64_t)a.ld << a.pc.lgP) + KT - 1) / KT);
+  int Wt = token_pieces(a.pc, a.S);
+  const bool solo = solo_waves(a.pc, a.S) || (Wt >= WAVES && blocks * tiles <= Wt);
+  if (solo) Wt &= ~(WAVES - 1);
+  else Wt = (int)std::max<int64_t>(1, std::min<int64_t>(Wt, blocks * (kStart + tiles) / (kStart + WAVES)));
   const int nt = Wt * a.pc.Hkv, Wp = prompt_pieces(a.pc), np = prompts ? Wp * a.pc.Hkv : 0;
   const dim3 grid((solo ? nt / WAVES : nt) + (prompts ? 1 : 0));
   if (solo)
@@ -1395,7 +1412,7 @@ hipError_t launch_page_attend(const PageAttendArgs& a, int q_dt, int max_q, bool
     set_last_kernel("page_valu");
     return launch_page_valu(a, q_dt, st);
   }
-  set_last_kernel((int64_t)max_q * a.G > 16 ? "page_prompt" : "page_tokens");
+  set_last_kernel((int64_t)max_q * a.G > 16 * kFewBlocks ? "page_prompt" : "page_tokens");
 #define UC_MATRIX(DIM, NGR) \
   q_dt == UC_BF16 ? launch_matrix<DIM, NGR, 1>(a, max_q, ws, st) : launch_matrix<DIM, NGR, 2>(a, max_q, ws, st)
   if (a.pc.D == 128) {

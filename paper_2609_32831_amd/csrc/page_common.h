@@ -39,8 +39,9 @@ struct PageAttendArgs {
   float scale_log2;
 };
 
-// units of work of a sequence of single tokens beside its tiles of 64 rows
-constexpr int kStart = 8;
+// blocks of 16 query rows of a KV head up to which a sequence counts as single
+// tokens, and units of work of such a block beside its tiles of 64 rows
+constexpr int kFewBlocks = 4, kStart = 8;
 
 // a bf16 in the low / high half of a word
 __device__ inline float word_step(uint32_t w) { return __uint_as_float(w << 16); }

@@ -227,6 +227,10 @@ ATTEND = [
     (8, 8, 64, 64, 128, "bf16", [500, 1, 1300], [16, 1, 9]),
     (16, 1, 128, 128, 256, "f16", [2049, 70], [1, 1]),
     (3, 3, 128, 32, 1024, "bf16", [3000], [5]),
+    # several blocks of 16 query rows (G * tokens of 17 to 64), some that see nothing
+    (28, 4, 128, 64, 16, "bf16", [700, 3, 64, 1300, 2], [3, 5, 9, 1, 9]),
+    (16, 4, 128, 32, 64, "f16", [129, 5000, 40], [16, 5, 12]),
+    (4, 1, 64, 64, 32, "bf16", [1000, 0, 16], [15, 2, 16]),
     # prompts: whole, chunked, one among single tokens, longer than the cache's rows (rows that see nothing)
     (4, 1, 64, 64, 16, "bf16", [130], [130]),
     (28, 4, 128, 64, 64, "bf16", [200, 333, 64], [200, 37, 3]),
@@ -283,7 +287,7 @@ def test_attention(case, path):
     got = run_attend(cache, table, lens, tokens, Hq, dtype, 7, path=uc.UC_PATH_VALU if path == "valu" else None)
     name = uc.uc_last_kernel()
     assert name == ("page_valu" if path == "valu" else
-                    "page_tokens" if max(tokens) * (Hq // Hkv) <= 16 else "page_prompt"), name
+                    "page_tokens" if max(tokens) * (Hq // Hkv) <= 64 else "page_prompt"), name
     check(*got, dtype)
 
 
@@ -317,7 +321,8 @@ def test_many_sequences(tokens):
     check(*run_attend(cache, table, lens, toks, 4, "bf16", 5), "bf16")
 
 
-@pytest.mark.parametrize("dtype,D,group,tokens", [("bf16", 128, 64, 1), ("f16", 128, 32, 40), ("bf16", 64, 32, 3)])
+@pytest.mark.parametrize("dtype,D,group,tokens", [("bf16", 128, 64, 1), ("f16", 128, 32, 40), ("bf16", 64, 32, 3),
+                                                  ("bf16", 128, 128, 21)])
 def test_a_piece_of_the_line_for_every_wave(dtype, D, group, tokens):
     """Many short sequences, three of them long enough to be cut, one with a
     page outside the cache, some without tokens or rows."""
@@ -378,7 +383,7 @@ def check_sized(cache, q, start, lens, table, scale, o, lse, dtype):
     want, want_lse = ref.attend(cache, f64(q), start, lens, table, scale)
     for s, n in enumerate(np.diff(start)):
         at = slice(start[s], start[s + 1])
-        few = n * (q.shape[1] // cache.Hkv) <= 16
+        few = n * (q.shape[1] // cache.Hkv) <= 64
         size, d_size, d_lse = (x[at] for x in ref.sizes(cache, f64(q), start, lens, table, scale, want_lse,
                                                         cache.D * 2.0 ** -24 * (22 if few else 1)))
         tiny = 2.0 ** -25 if dtype == "f16" else 2.0 ** -126
@@ -459,7 +464,7 @@ def test_queries_of_far_sizes(tokens, dtype):
 
 
 @pytest.mark.parametrize("path", ["auto", "valu"])
-@pytest.mark.parametrize("tokens", [1, 24])
+@pytest.mark.parametrize("tokens", [1, 24, 40])
 def test_pages_outside_the_cache(tokens, path):
     """An entry outside the cache spoils its own sequence only."""
     lens = [100, 200, 100]
