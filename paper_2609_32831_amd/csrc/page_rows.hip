@@ -12,9 +12,10 @@
 // Bound by bytes: 2 D elements in and D + 8 NG bytes out per row and head.
 // 16 lanes (D = 128) or 8 (D = 64) take a row's keys and values, 8 channels of
 // each: one 16-byte load of 16-bit rows, one 4-byte store of codes.  16001 rows
-// of 4 heads of 128 bf16 (42 MB): append 15.8 us, read 8.8 us.  The append is
-// still held up by its arithmetic, some 150 instructions for 16 elements (true
-// divisions: 18.6 us; keys and values by different threads 16.4).
+// of 4 heads of 128 bf16 (42 MB): append 14.1 us, read 8.7 us.  The append is
+// still held up by its arithmetic, some 11 instructions an element (with true
+// divisions 18.6 us; keys and values by different threads 16.4; every element
+// held to its bounds 15.6).
 #include "page_common.h"
 
 namespace uc {
@@ -107,14 +108,21 @@ __global__ __launch_bounds__(256) void page_append_kernel(RowArgs a, int row_blo
   }
   const bool live = slot >= 0 && (slot >> pc.lgP) < pc.n_pages;
   const int64_t row = live ? page_row(slot >> pc.lgP, pc.Hkv, h, pc.lgP, slot) : 0;
-  const int per = LANES / ng;  // lanes of one group
+  const int lg = __builtin_ctz(LANES) - __builtin_ctz(ng), per = 1 << lg;  // lanes of one group
 #pragma unroll
   for (int kv = 0; kv < 2; ++kv) {
     float(&y)[8] = x[kv];
-    float lo = INFINITY, hi = -INFINITY;
+    // a NaN or what passes the bound has larger bits than the bound
+    uint32_t most = 0;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      y[e] = y[e] != y[e] ? 0.0f : fminf(fmaxf(y[e], -kMost), kMost);
+    for (int e = 0; e < 8; ++e) most = max(most, __float_as_uint(y[e]) & 0x7FFFFFFFu);
+    if (__builtin_amdgcn_ballot_w64(most > __float_as_uint(kMost))) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) y[e] = y[e] != y[e] ? 0.0f : fminf(fmaxf(y[e], -kMost), kMost);
+    }
+    float lo = y[0], hi = y[0];
+#pragma unroll
+    for (int e = 1; e < 8; ++e) {
       lo = fminf(lo, y[e]);
       hi = fmaxf(hi, y[e]);
     }
@@ -147,7 +155,7 @@ __global__ __launch_bounds__(256) void page_append_kernel(RowArgs a, int row_blo
     uint32_t* codes = (uint32_t*)(kv ? pc.codes_v : pc.codes_k);
     uint32_t* scale = (uint32_t*)(kv ? pc.scale_v : pc.scale_k);
     codes[row * (D / 8) + (kv ? code_word<D, false>(c) : code_word<D, true>(c))] = w;
-    if (c % per == 0) scale[row * ng + c / per] = (sb >> 16) | (mb << 16);
+    if ((c & (per - 1)) == 0) scale[row * ng + (c >> lg)] = (sb >> 16) | (mb << 16);
   }
 }
 
