@@ -681,7 +681,7 @@ uc_status uc_page_read(const uc_page_cache* cache, const int32_t* slots, int T, 
  * a query that sees no row gets o = 0 and lse = -inf.
  *   q       token t's head h at q + t * q_ld + h * D (q_dt; q_ld >= Hq * D, a
  *           multiple of 8, 4 for UC_F32; 16-byte aligned)
- *   o       [T, Hq, D] of q_dt, 16-byte aligned
+ *   o       [T, Hq, D] of q_dt, 16-byte aligned, not overlapping q
  *   lse     optional float [T, Hq]: natural-log log-sum-exp of the logits
  *   max_q   at least the largest n; a sequence with more tokens may be left out
  * Rows of any size may lie behind those that a query sees.  A query that sees

@@ -565,6 +565,16 @@ def _ints(at: int, *ts: Optional[torch.Tensor]):
                              t.get_device() == at), "int32, contiguous, on one device"
 
 
+def _ws_on(nbytes: int, device, stream) -> torch.Tensor:
+    """A workspace of the stream that the call goes to, which alone may use the
+    memory again when the call has returned."""
+    if stream is None:
+        return _ws(nbytes, device)
+    assert isinstance(stream, torch.cuda.Stream), "a stream's bare handle needs a workspace given"
+    with torch.cuda.stream(stream):
+        return _ws(nbytes, device)
+
+
 def _token_rows(x: torch.Tensor, y: torch.Tensor, T: int, heads: int, D: int) -> int:
     """x and y [T, heads, D] with the heads of a token together, alike in
     everything; the distance of two tokens in elements."""
@@ -585,7 +595,7 @@ def uc_page_free(table: torch.Tensor, len: torch.Tensor, page_rows: int, free_li
     n_pages = free_list.numel()
     assert len.numel() == S and pool.numel() == 2
     if ws is None:
-        ws = _ws(lib.uc_page_free_workspace_size(n_pages), table.device)
+        ws = _ws_on(lib.uc_page_free_workspace_size(n_pages), table.device, stream)
     _check(lib.uc_page_free(S, page_rows, n_pages, table.data_ptr(), nb, len.data_ptr(),
                             free_list.data_ptr(), pool.data_ptr(), ws.data_ptr(), ws.numel(),
                             _stream(stream)), "uc_page_free")
@@ -658,7 +668,7 @@ def uc_page_attend(cache: PageCache, q: torch.Tensor, q_start: torch.Tensor, len
                            lse.numel() == T * Hq and lse.get_device() == at)
     assert q.get_device() == o.get_device() == at, "on the cache's device"
     if ws is None:
-        ws = _ws(lib.uc_page_attend_workspace_size(cache._ref, Hq, T, S, max_q), q.device)
+        ws = _ws_on(lib.uc_page_attend_workspace_size(cache._ref, Hq, T, S, max_q), q.device, stream)
     _check(lib.uc_page_attend(cache._ref, Hq, q.data_ptr(), TORCH_DT[q.dtype], ld, T, S, max_q,
                               q_start.data_ptr(), len.data_ptr(), table.data_ptr(), nb, sm_scale,
                               o.data_ptr(), _ptr(lse), ws.data_ptr(), ws.numel(),
@@ -690,7 +700,7 @@ def uc_beam_select(logits: torch.Tensor, score: torch.Tensor, done: Optional[tor
                              t.get_device() == at)
     assert score.numel() == score_out.numel() == parent.numel() == token.numel() == n
     if ws is None:
-        ws = _ws(lib.uc_beam_select_workspace_size(R, W, V), logits.device)
+        ws = _ws_on(lib.uc_beam_select_workspace_size(R, W, V), logits.device, stream)
     _check(lib.uc_beam_select(R, W, V, logits.data_ptr(), TORCH_DT[logits.dtype], ld,
                               score.data_ptr(), _ptr(done), eos, pad, score_out.data_ptr(),
                               parent.data_ptr(), token.data_ptr(), _ptr(done_out), ws.data_ptr(),

@@ -179,6 +179,10 @@ uc_status uc_page_attend(const uc_page_cache* cache, int Hq, const void* q, uc_d
   if ((st = check_rows("q", q, q_dt, q_ld, (int64_t)Hq * pc.D)) ||
       (st = check_rows("o", o, q_dt, (int64_t)Hq * pc.D, (int64_t)Hq * pc.D)))
     return st;
+  const char *q0 = (const char*)q, *o0 = (const char*)o;
+  const int64_t size = q_dt == UC_F32 ? 4 : 2, row = (int64_t)Hq * pc.D;
+  if (q0 < o0 + T * row * size && o0 < q0 + ((T - 1) * q_ld + row) * size)
+    return fail(UC_E_INVALID, "q and o overlap");
   if (lse && !aligned4(lse)) return fail(UC_E_INVALID, "lse is not 4-byte aligned");
   const size_t need = page_attend_workspace(pc, Hq / pc.Hkv, S, max_q);
   if (!ws || !aligned16(ws) || ws_bytes < need)

@@ -191,7 +191,7 @@ __global__ __launch_bounds__(256) void beam_rows_kernel(SelectArgs a) {
   if (a.done && a.done[row]) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), W = a.W;
   const char* p = (const char*)a.logits + (int64_t)row * a.ld * EB;
-  const int first = split * a.span, end = min(a.V, first + a.span);
+  const int first = split * a.span, end = first + min(a.V - first, a.span);
   // whole 16-byte vectors from `from` on; single elements before and behind
   const int from = min(end, first + (int)(((16 - ((uintptr_t)(p + (int64_t)first * EB) & 15)) & 15) / EB));
   const int vecs = (end - from) / N, to = from + vecs * N;

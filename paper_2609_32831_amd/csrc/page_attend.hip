@@ -37,6 +37,7 @@ constexpr int WAVES = 4;
 constexpr int KT = 64;         // keys per tile
 constexpr float kLazy = 8.0f;  // base-2 headroom before the reference maximum is raised
 constexpr float kNone = -3.0e38f;  // the reference maximum before any visible key
+constexpr float kFar = 0x1p16f;    // references beyond it: their own rounding counts
 
 struct Seq {
   int q0, n, len;
@@ -564,14 +565,14 @@ __global__ __launch_bounds__(256, 2) void page_tokens_kernel(PageAttendArgs a, i
           mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
           const float m_new = fmaxf(m, mx), alpha = __builtin_amdgcn_exp2f(m - m_new);
           m = m_new;
-          far = __builtin_amdgcn_ballot_w64(m > 0x1p22f) != 0;
+          far = __builtin_amdgcn_ballot_w64(fabsf(m) > kFar) != 0;
           l *= alpha;
 #pragma unroll
           for (int g = 0; g < NG; ++g) low[g] *= alpha;
 #pragma unroll
           for (int d = 0; d < DT; ++d) acc[d] *= alpha;
         }
-        if (far) {  // m's own rounding may reach the exponent's range: round the others alike
+        if (far) {  // round the others alike
 #pragma unroll
           for (int e = 0; e < 16; ++e) p[e] = scaled_less(p[e], a.scale_log2, m);
         } else {
@@ -731,9 +732,10 @@ __global__ __launch_bounds__(256, 2) void page_tokens_kernel(PageAttendArgs a, i
 // power of two).
 //
 // Rows of more different sizes within 16 (one of infinities, say, that earlier
-// queries do not see), and values beyond 2^-60 .. 2^76, mark the workgroup's
-// piece; every block that has a part in it is computed anew from the cache, a
-// row per workgroup.  Looking for them costs 2 % of the kernel's time.
+// queries do not see), values beyond 2^-60 .. 2^76 and logits beyond 2^16 mark
+// the workgroup's piece; every block that has a part in it is computed anew from
+// the cache, a row per workgroup: right, but a hundred times as slow.  Looking
+// for them costs 2 % of the kernel's time.
 //
 // Four prompts of 1500 tokens over up to 8192 rows, 28 query heads on 4, D 128
 // (342 GFLOP): 460 us a call, 745 TFLOP/s.  A stage of 64 keys x 32 rows is 76
@@ -1130,6 +1132,7 @@ __global__ __launch_bounds__(64 * PWAVES, 2) void page_prompt_kernel(PageAttendA
               if (mx > m[c] + 5.0f) {  // (eight weights above 256 together: one above 2^5)
                 const float alpha = __builtin_amdgcn_exp2f(m[c] - mx);
                 m[c] = mx;
+                if (fabsf(mx) > kFar) s_wide = 1;  // it would swallow e
                 l[c] *= alpha;
                 low[c] *= alpha;
 #pragma unroll

@@ -9,6 +9,7 @@ import torch
 import paper_2609_32831_amd as uc
 
 FAKE = 0x100000  # aligned non-null address; validation never dereferences it
+FAR = 0x10000000000000  # and one that no other argument reaches
 E, U, W = uc.UC_E_INVALID, uc.UC_E_UNSUPPORTED, uc.UC_E_WORKSPACE
 L = uc.lib
 
@@ -40,7 +41,7 @@ APPEND = dict(cache=cache(), k=FAKE, v=FAKE, dt=uc.UC_BF16, ld=512, T=5, slots=F
               stream=None)
 READ = dict(cache=cache(), slots=FAKE, T=5, k=FAKE, v=FAKE, dt=uc.UC_BF16, ld=512, stream=None)
 ATTEND = dict(cache=cache(), Hq=28, q=FAKE, dt=uc.UC_BF16, q_ld=28 * 128, T=5, S=3, max_q=3, q_start=FAKE, len=FAKE,
-              table=FAKE, ld=8, sm_scale=0.1, o=FAKE, lse=FAKE, ws=FAKE, ws_bytes=1 << 40, stream=None)
+              table=FAKE, ld=8, sm_scale=0.1, o=FAR, lse=FAKE, ws=FAKE, ws_bytes=1 << 40, stream=None)
 SELECT = dict(R=2, W=4, V=1000, logits=FAKE, dt=uc.UC_BF16, ld=1000, score=FAKE, done=FAKE, eos=2, pad=0,
               score_out=FAKE, parent=FAKE, token=FAKE, done_out=FAKE, ws=FAKE, ws_bytes=1 << 30, stream=None)
 REORDER = dict(R=2, W=4, parent=FAKE, token=FAKE, table=FAKE, ld=8, len=FAKE, page_rows=64, table_out=FAKE,
@@ -72,6 +73,8 @@ CASES = [
       (dict(T=(1 << 25) + 1), U)]),
     ("uc_page_attend", ATTEND, rows("q", "o") + ints("q_start", "len", "table") +
      [(dict(Hq=0), E), (dict(Hq=30), E), (dict(dt=9), E), (dict(q_ld=28 * 128 - 8), E), (dict(q_ld=28 * 128 + 4), E),
+      (dict(o=FAKE), E), (dict(o=FAKE + 5 * 28 * 256 - 16), E), (dict(o=FAKE - 16), E),
+      (dict(q_ld=28 * 128 + 64, o=FAKE + 28 * 256), E),
       (dict(T=-1), E), (dict(S=0), E), (dict(max_q=0), E), (dict(ld=0), E), (dict(lse=FAKE + 2), E),
       (dict(sm_scale=0.0), E), (dict(sm_scale=-1.0), E), (dict(sm_scale=float("nan")), E),
       (dict(sm_scale=float("inf")), E), (dict(sm_scale=3e38), E), (dict(T=1 << 27), U), (dict(ld=1 << 30), U),

@@ -446,6 +446,23 @@ def test_infinite_rows_that_earlier_queries_do_not_see(tokens, D, group):
         check(o[a:b], lse[a:b], want[a:b], want_lse[a:b], "bf16")
 
 
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("tokens", [4, 20, 70])
+def test_equal_keys_of_far_logits(tokens, sign):
+    """Every key alike, logits of +-2^31: all weights are the same."""
+    lens, Hkv, G, D = [300], 2, 2, 128
+    cache, table = make_cache(lens, 16, Hkv, D, 64, 66)
+    r = np.random.default_rng(67)
+    k = np.broadcast_to(np.float32(2.0 ** 27), (300, Hkv, D))
+    put_rows(cache, table, 0, range(300), k, r.standard_normal((300, Hkv, D)))
+    q = torch.full((tokens, Hkv * G, D), 1.375 * sign, device="cuda").bfloat16()
+    o, lse = torch.empty_like(q), torch.empty(tokens, Hkv * G, device="cuda")
+    uc.uc_page_attend(cache.device(uc), q, i32([0, tokens]), i32(lens), i32(table), tokens, 0.1, o, lse)
+    want, want_lse = ref.attend(cache, f64(q), [0, tokens], lens, table, float(np.float32(0.1)))
+    check(o, torch.zeros_like(lse), want, np.zeros_like(want_lse), "bf16")
+    assert np.allclose(f64(lse), want_lse, rtol=1e-5)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])
 @pytest.mark.parametrize("tokens", [4, 70])
 def test_queries_of_far_sizes(tokens, dtype):
@@ -725,7 +742,7 @@ def test_attention_on_another_stream():
         o2, lse2 = torch.zeros_like(q), torch.zeros(63, 6, device="cuda")
         s.wait_stream(torch.cuda.current_stream())
         if given:
-            run(o2, lse2, stream=s)
+            run(o2, lse2, None, stream=s)  # with a workspace of its own
         else:
             with torch.cuda.stream(s):
                 run(o2, lse2)
