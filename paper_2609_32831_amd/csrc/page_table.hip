@@ -56,34 +56,38 @@ __global__ __launch_bounds__(1024) void page_count_kernel(const uint8_t* __restr
   if (threadIdx.x == 0) count[blockIdx.x] = total;
 }
 
-// Unmarked pages to the list: one workgroup for all (count null), or one for
-// every kListPages, behind the counts of those before it.
+// Unmarked pages to the list: one workgroup for every kListPages, behind those
+// of the ranges before it (count null: counted here, every workgroup for
+// itself).
 __global__ __launch_bounds__(1024) void page_list_kernel(const uint8_t* __restrict__ mark, int n_pages,
                                                          const int32_t* __restrict__ count,
                                                          int32_t* __restrict__ list, int32_t* __restrict__ pool) {
   __shared__ int part[16];
-  int base = 0, all = 0;
+  int base, all, total, before = 0, sum = 0;
+  const int p0 = blockIdx.x * kListPages, p1 = min(n_pages, p0 + kListPages);
+  const int first = p0 + threadIdx.x * 16;
+  const uint32_t open = open_pages(mark, first, n_pages);
   if (count) {
-    int before = 0, sum = 0, total;
     for (int i = threadIdx.x; i < (int)gridDim.x; i += 1024) {
       sum += count[i];
       if (i < (int)blockIdx.x) before += count[i];
     }
-    block_scan(before, part, base);
-    block_scan(sum, part, total);
-    all = total;
+  } else {
+#pragma unroll 4
+    for (int b = 0; b < (int)gridDim.x; ++b) {
+      const int at = b * kListPages + threadIdx.x * 16;
+      if (at >= n_pages) break;
+      const uint4 v = *reinterpret_cast<const uint4*>(mark + at);  // (bytes of 0 and 1, zeros behind the last)
+      const int free = min(16, n_pages - at) - (__popc(v.x) + __popc(v.y) + __popc(v.z) + __popc(v.w));
+      sum += free;
+      if (b < (int)blockIdx.x) before += free;
+    }
   }
-  const int p0 = count ? blockIdx.x * kListPages : 0, p1 = count ? min(n_pages, p0 + kListPages) : n_pages;
-  for (int p = p0; p < p1; p += kListPages) {
-    const int first = p + threadIdx.x * 16;
-    const uint32_t open = open_pages(mark, first, n_pages);
-    int total;
-    const int upto = block_scan((int)__popc(open), part, total);
-    int at = base + upto - __popc(open);
-    for (uint32_t left = open; left; left &= left - 1) list[at++] = first + __ffs(left) - 1;
-    base += total;
-  }
-  if (!count) all = base;
+  block_scan(before, part, base);
+  block_scan(sum, part, all);
+  const int upto = block_scan((int)__popc(open), part, total);
+  int at = base + upto - __popc(open);
+  for (uint32_t left = open; left; left &= left - 1) list[at++] = first + __ffs(left) - 1;
   // -1 behind the last: every workgroup the entries of its own range
   for (int i = max(all, p0) + threadIdx.x; i < p1; i += 1024) list[i] = -1;
   if (blockIdx.x == 0 && threadIdx.x == 0) {
@@ -239,8 +243,12 @@ size_t page_free_workspace(int n_pages) {
   return mark_bytes(n_pages) + (((size_t)list_blocks(n_pages) * sizeof(int32_t) + 255) & ~(size_t)255);
 }
 
-// Three launches, four where the pages are many: 65536 pages in one workgroup
-// are four passes of two microseconds and more.
+// Three launches, four where the pages are very many: up to kFewRanges ranges
+// it is cheaper that every workgroup of the list counts the pages before its
+// own than that a launch does (a table of 1000 sequences over 9 ranges, with the
+// step behind it: 23.0 us, and 26.3 with the launch; 200000 pages alone 16.3 and
+// 15.7, 400000 21.5 and 16.0).
+constexpr int kFewRanges = 12;
 hipError_t launch_page_free(const int32_t* table, const int32_t* len, int S, int ld, int lgP,
                             int n_pages, int32_t* list, int32_t* pool, void* ws, hipStream_t st) {
   if ((int64_t)S * ld <= kSmallEntries && n_pages <= kSmallPages) {
@@ -254,8 +262,8 @@ hipError_t launch_page_free(const int32_t* table, const int32_t* len, int S, int
   hipLaunchKernelGGL(page_mark_kernel, dim3((ld + 255) / 256, min(S, 65535)), dim3(256), 0, st, table, len,
                      S, ld, lgP, n_pages, mark);
   const int blocks = list_blocks(n_pages);
-  if (blocks <= 1) {
-    hipLaunchKernelGGL(page_list_kernel, dim3(1), dim3(1024), 0, st, mark, n_pages, nullptr, list, pool);
+  if (blocks <= kFewRanges) {
+    hipLaunchKernelGGL(page_list_kernel, dim3(blocks), dim3(1024), 0, st, mark, n_pages, nullptr, list, pool);
   } else {
     int32_t* count = (int32_t*)(mark + mark_bytes(n_pages));
     hipLaunchKernelGGL(page_count_kernel, dim3(blocks), dim3(1024), 0, st, mark, n_pages, count);

@@ -171,6 +171,7 @@ def test_copies_join_the_append():
 TABLES = [  # S, P, most rows, most new, free pages to spare, table columns to spare, slots to spare
     (1, 16, 0, 1, 1, 0, 0), (5, 16, 40, 3, 50, 1, 4), (70, 64, 900, 300, 400, 2, 0), (300, 32, 500, 40, 200, 0, 9),
     (1500, 16, 90, 2, 100, 1, 3), (33, 256, 5000, 700, 9, 0, -50), (9, 16, 30000, 20000, 5000, 0, 1),
+    (1200, 16, 700, 2, 3000, 1, 0), (40, 16, 900, 30, 33000, 0, 0), (60, 16, 900, 30, 240001, 0, 0),
 ]
 
 
