@@ -9,9 +9,11 @@
 // the elements that pass a floor, which W elements are known to reach, and
 // raises the floor when its list is full; so an element costs a multiply-add,
 // an exponential, an addition and its share of a comparison.  384 rows of
-// 131071 bf16 (87 MB but for the beams that ended): 28 us, 3.1 TB/s.  (W best
+// 131071 bf16 (87 MB without the beams that ended): 28 us, 3.1 TB/s.  (W best
 // kept in order in the wave's lanes instead: 49 us.)  The choice among the
-// candidates takes 8 us, most of it W dependent steps over a wave.
+// candidates takes 8 us, most of it W dependent steps over a wave.  A whole
+// selection of 384 live rows: 35 us, 43 where a mask leaves one logit in a
+// thousand, 700 where rows rise all along.
 //
 // Reordering.  A beam's pages before the one being filled are full and may be
 // shared; that last page is each beam's own.  The first child of a beam keeps
@@ -80,8 +82,11 @@ struct KeyStep {
   }
 };
 
-// What a wave has gathered (LDS), and what an element has to pass to join: W
-// elements of the split have a value of v or more, or key or more.
+// What a wave has gathered (LDS), and what an element has to reach to join: W
+// elements of the split have keys of `key` or more.  v is the value below which
+// none can: that of `key`, or the next above it where `key` is one that the
+// wave has read, since its later vectors have larger indexes (a mask leaves
+// most logits of a row equal).
 constexpr int kCap = 576;  // W and eight elements of 64 lanes
 struct Floor {
   float v;
@@ -107,7 +112,7 @@ __device__ inline void cut_down(uint64_t* g, Floor& f, int W, int lane) {
   }
   __builtin_amdgcn_wave_barrier();
   if (lane < W) g[lane] = mine;
-  f.v = value_of(f.key);
+  f.v = value_of((f.key | 0xFFFFFFFFu) + 1);
   f.count = W;
   __builtin_amdgcn_wave_barrier();
 }
@@ -247,6 +252,7 @@ __global__ __launch_bounds__(256) void beam_rows_kernel(SelectArgs a) {
     const bool in = lane < n_edge;
     const int at = in ? (lane < n_head ? first + lane : to + lane - n_head) : 0;
     float x[1] = {in ? load_elem(p, DT, at) : -INFINITY};
+    f.v = value_of(f.key);  // (indexes before the vectors' among them)
     consume<1>(x, at, in, W, lane, g, f, r, s);
   }
   // the wave's sum, then the workgroup's lists and sums

@@ -631,6 +631,20 @@ def test_beam_selection_of_special_rows():
     check_beams(select(torch.from_numpy(x).cuda(), torch.from_numpy(score).cuda(), torch.from_numpy(done).cuda(), -1, 1), want)
 
 
+@pytest.mark.parametrize("low", [-np.inf, float(torch.finfo(torch.bfloat16).min), 0.5])
+def test_beam_selection_of_masked_rows(low):
+    """Most logits of a row alike: what a mask leaves, and ties by the index."""
+    r = np.random.default_rng(81)
+    x = np.full((3, 4, 20011), low, np.float32)
+    for i in range(3):
+        at = r.permutation(20011)[:(0, 3, 40)[i]]
+        x[i][:, at] = r.standard_normal((4, len(at))) * 2
+    x = torch.from_numpy(x).cuda().bfloat16()
+    score = np.array([[0.0, -0.5, -1.0, -1.0]] * 3, np.float32)
+    want = ref.beam_select(f64(x), score.astype(np.float64), np.zeros((3, 4)), -1, 0)
+    check_beams(select(x, torch.from_numpy(score).cuda(), torch.zeros(3, 4, dtype=torch.uint8, device="cuda"), -1, 0), want)
+
+
 @pytest.mark.parametrize("order", ["rising", "falling"])
 def test_beam_selection_of_sorted_rows(order):
     x = np.linspace(-4, 4, 6000, dtype=np.float32)[None, None].repeat(3, 1)
