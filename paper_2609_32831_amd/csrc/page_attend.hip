@@ -171,6 +171,17 @@ __global__ __launch_bounds__(256) void page_attend_valu_kernel(PageAttendArgs a)
   }
 }
 
+// inclusive sums over the lanes, without LDS
+__device__ inline int wave_scan(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false);
+  return x;
+}
+
 // ---------------------------------------------------------------- the line of tiles
 // U units cut into W pieces that differ by one unit at most, the longer ones
 // first (a call has fewer than 2^31 units, checked on the host).
@@ -344,34 +355,49 @@ __global__ __launch_bounds__(256, 2) void page_tokens_kernel(PageAttendArgs a, i
   const int turn = SOLO ? 0 : wave;  // the wave's among a piece's tiles
   if (SOLO ? lane == 0 : threadIdx.x == 0) cuts[w * Hkv + h] = Cut{-1, 0, 0, 0};
 
-  // this piece of the line; lane i counts sequences i c .. i c + c - 1
-  const int c = (a.S + 63) / 64;
-  Seq x{0, 0, 0};
+  // This piece of the line: the units of 64 sequences at a time, a sum for each
+  // lane's c times 64, so that two looks find the sequence that holds unit u0.
+  const int c = (a.S + 4095) / 4096;
+  auto count = [&](int s, Seq& x) {
+    x = Seq{0, 0, 0};
+    if (s < a.S) x = seq_of(a, s);
+    return token_blocks(x, G) * (START + tiles_of(x.len));  // (no tokens: no blocks)
+  };
+  Seq x;
   int mine = 0;
-  for (int s = lane * c; s < min(a.S, (lane + 1) * c); ++s) {
-    x = seq_of(a, s);
-    mine += token_blocks(x, G) * (START + tiles_of(x.len));
+  if (a.S <= 64) {
+    mine = count(lane, x);
+  } else {
+#pragma unroll 4
+    for (int k = 0; k * 64 < a.S; ++k) {
+      const int sum = __builtin_amdgcn_readlane(wave_scan(count(k * 64 + lane, x)), 63);
+      if (lane == k / c) mine += sum;
+    }
   }
-  int upto = mine;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int y = __shfl_up(upto, o, 64);
-    if (lane >= o) upto += y;
-  }
+  int upto = wave_scan(mine);
   const int U = __builtin_amdgcn_readlane(upto, 63);
   if (U == 0) return;
   // a sequence and a tile per wave at least
   const Line line(U, max(1, min(W_all, U / (START + STEP))));
   if (w >= line.W) return;
   const int u0 = line.first(w), u1 = line.first(w + 1);
-  const int bucket = __builtin_ctzll(__builtin_amdgcn_ballot_w64(upto > u0));
-  int s = bucket * c, before = __builtin_amdgcn_readlane(upto - mine, bucket);  // units before sequence s
-  if (c == 1) {
-    x = Seq{__builtin_amdgcn_readlane(x.q0, bucket), __builtin_amdgcn_readlane(x.n, bucket),
-            __builtin_amdgcn_readlane(x.len, bucket)};
-  } else {
-    x = seq_of(a, s);
+  int at = __builtin_ctzll(__builtin_amdgcn_ballot_w64(upto > u0)), s = at;
+  int before = __builtin_amdgcn_readlane(upto - mine, at);  // units before sequence s
+  if (a.S > 64) {
+    for (s = at * c * 64;; s += 64) {
+      mine = count(s + lane, x);
+      upto = before + wave_scan(mine);
+      const int end = __builtin_amdgcn_readlane(upto, 63);
+      if (end > u0 || s + 64 >= a.S) break;
+      before = end;
+    }
+    const uint64_t past = __builtin_amdgcn_ballot_w64(upto > u0);
+    at = past ? __builtin_ctzll(past) : 0;
+    s += at;
+    before = __builtin_amdgcn_readlane(upto - mine, at);
   }
+  x = Seq{__builtin_amdgcn_readlane(x.q0, at), __builtin_amdgcn_readlane(x.n, at),
+          __builtin_amdgcn_readlane(x.len, at)};
   Lds& L = *reinterpret_cast<Lds*>(lds + wave * sizeof(Lds));
 
   // The block at hand, `blk` of the sequence's `blks`: tiles [t0, t1) of it lie

@@ -322,6 +322,17 @@ def test_many_sequences(tokens):
     check(*run_attend(cache, table, lens, toks, 4, "bf16", 5), "bf16")
 
 
+@pytest.mark.parametrize("S,Hkv", [(65, 4), (513, 1), (4096, 2), (4097, 1), (9000, 1)])
+def test_sequences_of_every_number(S, Hkv):
+    """The search for a piece's first sequence: 64 sequences a look, and more."""
+    r = np.random.default_rng(S)
+    lens = [int(x) for x in r.integers(0, 70, S)]
+    toks = [int(x) for x in r.integers(0, 2, S)]
+    lens[S - 1], toks[S - 1], lens[S // 2], toks[S // 2] = 300, 1, 500, 2
+    cache, table = make_cache(lens, 16, Hkv, 64, 32, S)
+    check(*run_attend(cache, table, lens, toks, 2 * Hkv, "bf16", 9), "bf16")
+
+
 @pytest.mark.parametrize("dtype,D,group,tokens", [("bf16", 128, 64, 1), ("f16", 128, 32, 40), ("bf16", 64, 32, 3),
                                                   ("bf16", 128, 128, 21)])
 def test_a_piece_of_the_line_for_every_wave(dtype, D, group, tokens):
