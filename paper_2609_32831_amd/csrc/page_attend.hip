@@ -1354,10 +1354,10 @@ __global__ __launch_bounds__(256, 8) void page_merge_kernel(PageAttendArgs a, in
 // workgroups per CU in one round, for prompts one (of twice the waves).  Where
 // the sequences are many, each of a single-token workgroup's waves has a piece:
 // then waves neither idle on sequences of fewer tiles than there are waves, nor
-// meet at the end of every sequence.  1024 sequences of 128 rows take 34 us
-// that way and 75 the other, 256 of 64 rows 12 and 21, 512 of 2048 rows 120 and
-// 136; but 128 of 1024 rows 30 and 25, and one of 65536 rows 131 and 124 (more
-// records to merge).
+// meet at the end of every sequence.  28 heads on 4, us that way and the other:
+// 1024 sequences of 128 rows 30 and 73, 512 of 2048 rows 123 and 142, 256 of 64
+// rows 10 and 21; but 256 of 512 rows 34 and 32, 128 of 1024 rows 30 and 25, one
+// of 65536 rows 66 and 33 (more records to merge).
 static int prompt_pieces(const PageCache& pc) { return std::max(1, device_cus() / pc.Hkv); }
 static bool solo_waves(const PageCache& pc, int S) { return S >= 2 * std::max(1, 2 * device_cus() / pc.Hkv); }
 static int token_pieces(const PageCache& pc, int S) {

@@ -40,7 +40,8 @@ struct PageAttendArgs {
 };
 
 // blocks of 16 query rows of a KV head up to which a sequence counts as single
-// tokens, and units of work of such a block beside its tiles of 64 rows
+// tokens, and units of work of such a block beside its tiles of 64 rows (5, 8,
+// 12 and 16: 64.9, 56.8, 59.1 and 59.6 us for 61 sequences of 1 to 40000 rows)
 constexpr int kFewBlocks = 4, kStart = 8;
 
 // a bf16 in the low / high half of a word
