@@ -349,7 +349,7 @@ def _tables(s):
     seq = torch.searchsorted(start[1:].contiguous(), i.int(), right=True)
     pos = n[seq] + i - start[seq]
     slot = torch.where(ok[seq], table[seq, pos // P] * P + pos % P, -1).int()
-    taken = torch.where(ok & (need > 0), upto, 0).amax()
+    taken = torch.where(ok, upto, 0).amax()
     one = torch.stack((torch.zeros_like(taken), is_free.sum()))
     return {"free": free, "pool": one.int(), "table": table, "len": torch.where(ok, n + s["new"], n).int(), "q_start": start,
             "slots": slot, "pool_out": torch.stack((taken, is_free.sum())).int(), "refused": (~ok).to(torch.uint8)}
