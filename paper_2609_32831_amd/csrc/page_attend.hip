@@ -754,8 +754,10 @@ __global__ __launch_bounds__(256, 2) void page_tokens_kernel(PageAttendArgs a, i
 // bits), is measured by what key j contributes whatever the values' sizes.  l
 // is summed in binary32 before that rounding.  The minima go through matrix
 // instructions of their own, q . k += sum_g m_g sum(q_g) with sum(q_g) in
-// three fp16 parts.  Queries enter as fp16 too, exactly (a row far from 1 by a
-// power of two).
+// three fp16 parts.  Queries enter as fp16 too, a row far from 1, or of sums
+// that fp16 does not hold, by a power of two: as such a row stands, its elements
+// below 2^-14 are off by 2^-25 at most, 2^-21 of its largest; the others are
+// exact.
 //
 // Rows of more different sizes within 16 (one of infinities, say, that earlier
 // queries do not see), values beyond 2^-60 .. 2^76 and logits beyond 2^16 mark
@@ -992,31 +994,48 @@ __global__ __launch_bounds__(64 * PWAVES, 2) void page_prompt_kernel(PageAttendA
       }
       most = fmaxf(most, __shfl_xor(most, 16, 64));
       most = fmaxf(most, __shfl_xor(most, 32, 64));
+      // sums of the groups' channels, all of them in every lane
+      float sq[NG];
+      auto add_up = [&]() {
+#pragma unroll
+        for (int n = 0; n < NG; ++n) sq[n] = 0.0f;
+#pragma unroll
+        for (int t = 0; t < KS; ++t)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) sq[t * NG / KS] += f[t][e];
+#pragma unroll
+        for (int n = 0; n < NG; ++n) {
+          sq[n] += __shfl_xor(sq[n], 16, 64);
+          sq[n] += __shfl_xor(sq[n], 32, 64);
+        }
+      };
+      add_up();
+      float most_sum = 0.0f;
+#pragma unroll
+      for (int n = 0; n < NG; ++n) most_sum = fmaxf(most_sum, fabsf(sq[n]));
       const int E = (int)(__float_as_uint(most) >> 23);  // 2^(E - 127) <= most
-      const bool far = most > 0.0f && (E < 127 - 4 || E > 127 + 14);
+      // elements and sums have to fit fp16: a row whose elements or sums reach
+      // 2^15 comes below 2, its sums below 2 D / NG
+      const bool far = most > 0.0f && (E < 127 - 4 || E > 127 + 14 || !(most_sum < 0x1p15f));
       const float out = far ? __uint_as_float((uint32_t)(254 - min(max(E, 1), 253)) << 23) : 1.0f;
       s_rows[c][threadIdx.x] = float2{__int_as_float(lim), far ? __uint_as_float((uint32_t)min(max(E, 1), 253) << 23) : 1.0f};
       scaled |= far;
-      float sq[NG];
+      if (__builtin_amdgcn_ballot_w64(far)) {
 #pragma unroll
-      for (int n = 0; n < NG; ++n) sq[n] = 0.0f;
+        for (int t = 0; t < KS; ++t)
 #pragma unroll
-      for (int t = 0; t < KS; ++t) {
+          for (int e = 0; e < 8; ++e) f[t][e] *= out;
+        add_up();  // anew: sums of large elements may have passed binary32
+      }
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          f[t][e] *= out;
-          sq[t * NG / KS] += f[t][e];
-        }
+      for (int t = 0; t < KS; ++t)
 #pragma unroll
         for (int e = 0; e < 4; ++e) qb[c][t][e] = h2(f[t][e], f[t][e + 4]);
-      }
       // sums in three fp16 parts: part g4 in this lane's slots
       uint32_t bits[4] = {0, 0, 0, 0};
 #pragma unroll
       for (int n = 0; n < NG; ++n) {
         float y = sq[n];
-        y += __shfl_xor(y, 16, 64);
-        y += __shfl_xor(y, 32, 64);
 #pragma unroll
         for (int p = 0; p < 2; ++p)
           if (p < g4) y -= f16_to_f32(f32_to_f16_bits(y));
