@@ -752,7 +752,11 @@ __global__ __launch_bounds__(256, 2) void page_tokens_kernel(PageAttendArgs a, i
 //   w_j = 2^(logit_j + e_j - m),  o ~ sum_j w_j (v_j 2^-e_j),  l = sum_j w_j 2^-e_j,
 // with the reference m kept over logit + e, so that w_j, rounded to fp16 (11
 // bits), is measured by what key j contributes whatever the values' sizes.  l
-// is summed in binary32 before that rounding.  The minima go through matrix
+// is summed in binary32 before that rounding.  The reference puts a row's
+// largest weight at 2^7 .. 2^15, so that the small ones of a long tail are fp16's
+// too: what lies below its subnormal step is off by 2^-32 of the largest (with
+// the largest at 1, a tail of 65500 keys of 2^-25.5 each, a 700th of the sum, was
+// lost from o and not from l).  The minima go through matrix
 // instructions of their own, q . k += sum_g m_g sum(q_g) with sum(q_g) in
 // three fp16 parts.  Queries enter as fp16 too, a row far from 1, or of sums
 // that fp16 does not hold, by a power of two: as such a row stands, its elements
@@ -773,6 +777,11 @@ __global__ __launch_bounds__(256, 2) void page_tokens_kernel(PageAttendArgs a, i
 // the rows (709 us); two buffers and a barrier per tile instead of the
 // pipeline of steps (530 us); bf16 planes (578 us); fixed orders of matrix and
 // vector instructions (498 to 553 us) - the compiler's own is the best.
+// A raised reference puts the largest weight at 2^kPeak; it is raised once a
+// weight passes 2^kRaise, which is looked at where the eight weights of a lane
+// together pass kTop = 8 * 2^kRaise, the last power that fp16 holds.
+constexpr float kPeak = 7.0f, kRaise = 12.0f, kTop = 0x1p15f;
+
 template <int D>
 constexpr int kRow = 2 * D + 32;  // bytes of a staged row: 8 consecutive rows start in different 8-bank groups
 
@@ -1151,7 +1160,7 @@ __global__ __launch_bounds__(64 * PWAVES, 2) void page_prompt_kernel(PageAttendA
           output(Vp, before_sub, p, 0, DT);
           const int r0 = t0 * KT + n * KEYS + sub * 32;
           const bool mask = always || r0 + 32 > lim_all;
-          if (__builtin_amdgcn_ballot_w64(mask || !(top[0] <= 256.0f && top[1] <= 256.0f))) {
+          if (__builtin_amdgcn_ballot_w64(mask || !(top[0] <= kTop && top[1] <= kTop))) {
             // rare: the step's products again (its keys are still there),
             // masked, against a reference raised where it has to be
             f4 s2[2][2];
@@ -1174,9 +1183,9 @@ __global__ __launch_bounds__(64 * PWAVES, 2) void page_prompt_kernel(PageAttendA
               }
               mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
               mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-              if (mx > m[c] + 5.0f) {  // (eight weights above 256 together: one above 2^5)
-                const float alpha = __builtin_amdgcn_exp2f(m[c] - mx);
-                m[c] = mx;
+              if (mx > m[c] + kRaise) {
+                const float m_new = mx - kPeak, alpha = __builtin_amdgcn_exp2f(m[c] - m_new);
+                m[c] = m_new;
                 if (fabsf(mx) > kFar) s_wide = 1;  // it would swallow e
                 l[c] *= alpha;
                 low[c] *= alpha;

@@ -12,7 +12,7 @@ if not torch.cuda.is_available():
 
 import paged_ref as ref  # noqa: E402
 import paper_2609_32831_amd as uc  # noqa: E402
-from test_gpu_paged import DT, _case, check_sized, i32, make_cache, put_rows  # noqa: E402
+from test_gpu_paged import DT, _case, check_sized, f64, half, i32, make_cache, put_rows  # noqa: E402
 
 
 # ---------------------------------------------------------------- queries
@@ -37,3 +37,42 @@ def test_queries_of_one_sign(tokens, size, D, group, dtype):
     uc.uc_page_attend(cache.device(uc), q, i32([0, tokens]), i32(lens), i32(table), tokens, 0.1, o, lse)
     assert torch.isfinite(o).all() and torch.isfinite(lse).all()
     check_sized(cache, q, [0, tokens], lens, table, float(np.float32(0.1)), o, lse, dtype)
+
+
+@pytest.mark.parametrize("peak", [100, 61000])
+@pytest.mark.parametrize("tokens,G", [(3, 1), (4096, 16)])
+def test_a_long_tail_under_a_peak(tokens, G, peak):
+    """One key takes nearly all, and some 65500 others, each of weight 2^-25.5
+    of it, take 2^-9.5 together.  Every value is 1 but the peak's, which is
+    zero, so the output is the tail's share.  (65536 query rows of a KV head:
+    as many blocks as there are pieces, so a piece holds most of a block's
+    rows.)
+
+    A prompt's weights are rounded to fp16: by 2^-12 of themselves, or by 2^-25
+    where they are subnormal, with the largest at 2^7 at least: n 2^-32 of the
+    values.  Single tokens: 2^-18 of the weights."""
+    _case(test="tail", tokens=tokens, G=G, peak=peak)
+    n, D, P = 65600, 64, 64
+    r = np.random.default_rng(peak)
+    one = 0x3F80 << 16  # a minimum of 1, steps of 0
+    pages = n // P
+    shape = (pages, 1, P, D // 2)
+    k, v = (torch.full((pages, 1, P, 1), w, dtype=torch.int32, device="cuda") for w in (0, one))
+    table = r.permutation(pages)
+    page = int(table[peak // P])
+    k[page, 0, peak % P], v[page, 0, peak % P] = one, 0
+    codes = torch.zeros(shape, dtype=torch.uint8, device="cuda")
+    q = torch.ones(tokens, G, D, device="cuda", dtype=torch.float16)
+    scale = np.float32(25.5 * np.log(2) / D)
+    o, lse = torch.empty_like(q), torch.empty(tokens, G, device="cuda")
+    uc.uc_page_attend(uc.PageCache(codes, codes, k, v), q, i32([0, tokens]), i32([n]), i32(table[None]), tokens,
+                      float(scale), o, lse)
+    logit = D * float(scale)
+    tail = (n - tokens + np.arange(tokens))[:, None] * np.exp(-logit)  # of the peak's weight
+    want, want_lse = (tail / (1 + tail))[..., None], logit + np.log1p(tail)
+    err = np.abs(f64(o) - want)
+    print(f"want {want.max():.3e} off {err.max():.3e}", flush=True)
+    # the logit of 17.7: sums of D terms of up to 22 times its size, by 2^-24 each
+    bound = (half("f16") + 2.0 ** -12 + logit * D * 22 * 2.0 ** -24) * want + n * 2.0 ** -32
+    assert np.all(err <= bound)
+    assert np.all(np.abs(f64(lse) - want_lse) <= 1e-5 * want_lse + 2.0 ** -12)
