@@ -717,8 +717,10 @@ size_t uc_page_attend_workspace_size(const uc_page_cache* cache, int Hq, int T, 
  *   done_out  optional uint8 [R, W]: done[parent], or token == eos
  * score_out may be score and done_out may be done.  1 <= W <= UC_MAX_BEAMS,
  * W <= V, W * V < 2^31, R * W <= 2^23, 0 <= pad < V; eos may be -1 (none).
- * Totals are formed in 64 bits from binary32 sums of exponentials.  ws:
- * uc_beam_select_workspace_size bytes. */
+ * Totals are formed in 64 bits from binary32 sums of exponentials, added in an
+ * order that goes by the index alone: beams of the same logits and score have
+ * the same totals.  (Logits of one beam that differ by less than the last bit of
+ * a total may come in either order.)  ws: uc_beam_select_workspace_size bytes. */
 uc_status uc_beam_select(int R, int W, int V, const void* logits, uc_dtype dt, int64_t ld,
                          const float* score, const uint8_t* done, int eos, int pad,
                          float* score_out, int32_t* parent, int32_t* token, uint8_t* done_out,

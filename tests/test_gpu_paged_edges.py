@@ -12,7 +12,7 @@ if not torch.cuda.is_available():
 
 import paged_ref as ref  # noqa: E402
 import paper_2609_32831_amd as uc  # noqa: E402
-from test_gpu_paged import DT, _case, check_sized, f64, half, i32, make_cache, put_rows  # noqa: E402
+from test_gpu_paged import DT, _case, check_beams, check_sized, f64, half, i32, make_cache, put_rows, select  # noqa: E402
 
 
 # ---------------------------------------------------------------- queries
@@ -76,3 +76,24 @@ def test_a_long_tail_under_a_peak(tokens, G, peak):
     bound = (half("f16") + 2.0 ** -12 + logit * D * 22 * 2.0 ** -24) * want + n * 2.0 ** -32
     assert np.all(err <= bound)
     assert np.all(np.abs(f64(lse) - want_lse) <= 1e-5 * want_lse + 2.0 ** -12)
+
+
+# ---------------------------------------------------------------- equal beams
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("R,W,V", [(2, 4, 1), (3, 4, 37), (2, 3, 1501), (2, 5, 32003), (40, 8, 4099), (1, 4, 131071)])
+def test_equal_beams_go_by_the_lower_index(R, W, V, dtype):
+    """Beams of the same logits and the same score have the same totals,
+    wherever in memory their rows begin, so the lower beam comes first."""
+    if W > V:
+        V = W
+    _case(test="equal_beams", R=R, W=W, V=V, dtype=dtype)
+    g = torch.Generator(device="cuda").manual_seed(V)
+    x = torch.randn(R, 1, V, generator=g, device="cuda") * 3
+    for pad in (0, 1, 3):  # rows further apart than they are long
+        y = torch.zeros(R, W, V + pad, device="cuda").to(DT[dtype])
+        y = y[:, :, pad:]
+        y.copy_(x.expand(R, W, V))
+        score = torch.full((R, W), -7.25, device="cuda")
+        done = torch.zeros(R, W, dtype=torch.uint8, device="cuda")
+        check_beams(select(y, score, done, -1, 0), ref.beam_select(f64(y), f64(score), done.cpu().numpy(), -1, 0))
