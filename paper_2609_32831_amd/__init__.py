@@ -577,13 +577,24 @@ def _ws_on(nbytes: int, device, stream) -> torch.Tensor:
 
 def _token_rows(x: torch.Tensor, y: torch.Tensor, T: int, heads: int, D: int) -> int:
     """x and y [T, heads, D] with the heads of a token together, alike in
-    everything; the distance of two tokens in elements."""
-    sx = x.stride()
+    everything (but the distances of single tokens and heads, which nothing
+    goes by); the distance of two tokens in elements."""
+    sx, sy = x.stride(), y.stride()
     assert x.shape == (T, heads, D) and sx[2] == 1 and (heads == 1 or sx[1] == D), \
         "[T, heads, D], a token's heads together"
-    assert x is y or (y.shape == x.shape and y.stride() == sx and y.dtype is x.dtype and
+    assert x is y or (y.shape == x.shape and sy[2] == 1 and (heads == 1 or sy[1] == D) and
+                      (T <= 1 or sy[0] == sx[0]) and y.dtype is x.dtype and
                       y.get_device() == x.get_device()), "keys and values differ in their layout"
     return sx[0] if T > 1 else heads * D
+
+
+def _logit_rows(x: torch.Tensor) -> int:
+    """The distance of the R * W rows of x [R, W, V] in elements."""
+    R, W, V = x.shape
+    s = x.stride()
+    assert (V == 1 or s[2] == 1) and (R == 1 or W == 1 or s[0] == W * s[1]), \
+        "rows of logits at one distance"
+    return s[1] if W > 1 else s[0] if R > 1 else V
 
 
 def uc_page_free(table: torch.Tensor, len: torch.Tensor, page_rows: int, free_list: torch.Tensor,
@@ -687,9 +698,7 @@ def uc_beam_select(logits: torch.Tensor, score: torch.Tensor, done: Optional[tor
     """The W best continuations of every request: logits [R, W, V] (rows at
     one distance), score [R, W] float, done [R, W] uint8 or None."""
     R, W, V = logits.shape
-    s = logits.stride()
-    assert s[2] == 1 and (R == 1 or s[0] == W * s[1]), "rows of logits at one distance"
-    ld = s[1] if W > 1 else s[0] if R > 1 else V
+    ld = _logit_rows(logits)
     at, n = logits.get_device(), R * W
     _ints(at, parent, token)
     for t in (score, score_out):
