@@ -851,12 +851,12 @@ const char* uc_status_string(uc_status s);
 /* Thread-local description of the calling thread's last error ("" if none). */
 const char* uc_last_error(void);
 /* Name of the main kernel the calling thread's last successful launch of
- * uc_attend_mixed, uc_attend_append, uc_attend_batch or uc_score_importance
- * ran ("decode_mfma", "decode_mfma_append", "prefill_mfma", "attend_wide",
- * "attend_valu", "decode_batch", "score_mfma", "score_wide", "score_valu"; ""
- * before any; "_wide" are the binary32 matrix-core kernels, "_valu" the
- * vector-ALU ones).  Lets tests assert the path a case reaches; static
- * storage, never freed. */
+ * uc_attend_mixed, uc_attend_append, uc_attend_batch, uc_score_importance or
+ * uc_page_attend ran ("decode_mfma", "decode_mfma_append", "prefill_mfma",
+ * "attend_wide", "attend_valu", "decode_batch", "score_mfma", "score_wide",
+ * "score_valu", "page_tokens", "page_prompt", "page_valu"; "" before any;
+ * "_wide" are the binary32 matrix-core kernels, "_valu" the vector-ALU ones).
+ * Lets tests assert the path a case reaches; static storage, never freed. */
 const char* uc_last_kernel(void);
 
 #ifdef __cplusplus

@@ -1447,7 +1447,7 @@ static void launch_matrix(const PageAttendArgs& a, int max_q, void* ws, hipStrea
                        merge_t, cuts_t, rec_t, cuts_p, rec_p, Wp, units, wide);
 }
 
-hipError_t launch_page_valu(const PageAttendArgs& a, int q_dt, hipStream_t st) {
+static void launch_page_valu(const PageAttendArgs& a, int q_dt, hipStream_t st) {
   const dim3 grid(std::min<uint32_t>((uint32_t)a.T * a.pc.Hkv * a.G, 1 << 20));
 #define UC_VALU(DIM, TYPE) \
   hipLaunchKernelGGL((page_attend_valu_kernel<DIM, TYPE>), grid, dim3(256), 0, st, a)
@@ -1461,18 +1461,14 @@ hipError_t launch_page_valu(const PageAttendArgs& a, int q_dt, hipStream_t st) {
     else UC_VALU(64, UC_F32);
   }
 #undef UC_VALU
-  return hipGetLastError();
 }
 
 hipError_t launch_page_attend(const PageAttendArgs& a, int q_dt, int max_q, bool valu, void* ws, hipStream_t st) {
-  if (valu) {
-    set_last_kernel("page_valu");
-    return launch_page_valu(a, q_dt, st);
-  }
-  set_last_kernel((int64_t)max_q * a.G > 16 * kFewBlocks ? "page_prompt" : "page_tokens");
 #define UC_MATRIX(DIM, NGR) \
   q_dt == UC_BF16 ? launch_matrix<DIM, NGR, 1>(a, max_q, ws, st) : launch_matrix<DIM, NGR, 2>(a, max_q, ws, st)
-  if (a.pc.D == 128) {
+  if (valu) {
+    launch_page_valu(a, q_dt, st);
+  } else if (a.pc.D == 128) {
     if (a.pc.ng == 4) UC_MATRIX(128, 4);
     else if (a.pc.ng == 2) UC_MATRIX(128, 2);
     else UC_MATRIX(128, 1);
@@ -1481,7 +1477,10 @@ hipError_t launch_page_attend(const PageAttendArgs& a, int q_dt, int max_q, bool
     else UC_MATRIX(64, 1);
   }
 #undef UC_MATRIX
-  return hipGetLastError();
+  const hipError_t e = hipGetLastError();
+  if (e == hipSuccess)
+    set_last_kernel(valu ? "page_valu" : (int64_t)max_q * a.G > 16 * kFewBlocks ? "page_prompt" : "page_tokens");
+  return e;
 }
 
 }  // namespace uc

@@ -1,9 +1,12 @@
-"""Layouts that the paged calls' binding takes, looked at before any launch (so
+"""Layouts that the paged calls' binding takes, and calls that launch nothing (so
 this runs without a GPU)."""
+import threading
+
 import pytest
 import torch
 
 import paper_2609_32831_amd as uc
+from test_abi_paged import ATTEND, L, call
 
 
 def test_a_single_token_has_no_distance():
@@ -33,3 +36,19 @@ def test_rows_of_logits_at_one_distance():
     for bad in (x[:, :2], x[..., ::2], x.transpose(1, 2)):
         with pytest.raises(AssertionError):
             uc._logit_rows(bad)
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="a launch has to fail, as it does without a GPU")
+def test_a_failed_launch_leaves_the_last_kernel():
+    got = []
+
+    def run():
+        for path in (uc.UC_PATH_AUTO, uc.UC_PATH_VALU):
+            prev = uc.uc_set_path(path)
+            got.append((call(L.uc_page_attend, ATTEND), uc.uc_last_kernel()))
+            uc.uc_set_path(prev)
+
+    t = threading.Thread(target=run)  # the name is the calling thread's: none yet
+    t.start()
+    t.join()
+    assert got == [(uc.UC_E_DEVICE, ""), (uc.UC_E_DEVICE, "")]
