@@ -626,8 +626,8 @@ typedef struct {
  * entries (at most table_ld; entries outside [0, n_pages) are passed over,
  * pages may be named more than once).  free_list [n_pages] receives the
  * others, ascending, -1 behind them, and pool [2] the pair (0, their count).
- * A sequence ends by its len becoming 0.  ws: uc_page_free_workspace_size
- * bytes. */
+ * A sequence ends by its len becoming 0.  S, table_ld <= 2^30.  ws:
+ * uc_page_free_workspace_size bytes. */
 uc_status uc_page_free(int S, int page_rows, int n_pages, const int32_t* table, int table_ld,
                        const int32_t* len, int32_t* free_list, int32_t* pool, void* ws,
                        size_t ws_bytes, void* stream);
@@ -649,7 +649,8 @@ size_t uc_page_free_workspace_size(int n_pages);
  *   pool_out [2] (entries taken up to, pool[1])
  *   refused  [S] bytes: 1 where refused
  * len_out may be len and pool_out may be pool; with others the call can be
- * repeated and gives the same.  All int32 (refused uint8), device. */
+ * repeated and gives the same.  S, table_ld, n_slots <= 2^30.  All int32
+ * (refused uint8), device. */
 uc_status uc_page_step(int S, int page_rows, int n_pages, const int32_t* len, const int32_t* new_len,
                        int32_t* table, int table_ld, const int32_t* free_list, const int32_t* pool,
                        int32_t* len_out, int32_t* q_start, int32_t* slots, int n_slots,
@@ -716,7 +717,7 @@ size_t uc_page_attend_workspace_size(const uc_page_cache* cache, int Hq, int T, 
  *   score_out [R, W] float, descending; parent, token [R, W] int32;
  *   done_out  optional uint8 [R, W]: done[parent], or token == eos
  * score_out may be score and done_out may be done.  1 <= W <= UC_MAX_BEAMS,
- * W <= V, W * V < 2^31, R * W <= 2^23, 0 <= pad < V; eos may be -1 (none).
+ * W <= V, W * V <= 2^30, R * W <= 2^23, 0 <= pad < V; eos may be -1 (none).
  * Totals are formed in 64 bits from binary32 sums of exponentials, added in an
  * order that goes by the index alone: beams of the same logits and score have
  * the same totals.  (Logits of one beam that differ by less than the last bit of

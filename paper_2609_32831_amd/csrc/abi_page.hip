@@ -37,6 +37,9 @@ namespace {
 // an append or a read: 16 heads' rows or more to a workgroup of 256, a page's
 // head to another; a launch holds fewer than 2^24 of them
 constexpr int64_t kMostRows = 1 << 27, kMostCopies = 1 << 22;
+// sequences, table columns, slots, and continuations of a request: what the
+// kernels' indexes pass by a grid's stride stays in 31 bits
+constexpr int kMostIndex = 1 << 30;
 
 bool aligned4(const void* p) { return ((uintptr_t)p & 3u) == 0; }
 
@@ -91,6 +94,8 @@ uc_status uc_page_free(int S, int page_rows, int n_pages, const int32_t* table, 
   uc_status st = check_paging(page_rows, n_pages);
   if (st) return st;
   if (S < 1 || table_ld < 1) return fail(UC_E_INVALID, "S and table_ld must be >= 1 (got %d, %d)", S, table_ld);
+  if (S > kMostIndex || table_ld > kMostIndex)
+    return fail(UC_E_UNSUPPORTED, "more than 2^30 sequences or table columns (got %d, %d)", S, table_ld);
   if ((st = check_ints("table", table)) || (st = check_ints("len", len)) ||
       (st = check_ints("free_list", free_list)) || (st = check_ints("pool", pool)))
     return st;
@@ -109,6 +114,8 @@ uc_status uc_page_step(int S, int page_rows, int n_pages, const int32_t* len, co
   if (st) return st;
   if (S < 1 || table_ld < 1 || n_slots < 0)
     return fail(UC_E_INVALID, "S and table_ld must be >= 1, n_slots >= 0 (got %d, %d, %d)", S, table_ld, n_slots);
+  if (S > kMostIndex || table_ld > kMostIndex || n_slots > kMostIndex)
+    return fail(UC_E_UNSUPPORTED, "more than 2^30 sequences, table columns or slots (got %d, %d, %d)", S, table_ld, n_slots);
   if ((st = check_ints("len", len)) || (st = check_ints("new_len", new_len)) || (st = check_ints("table", table)) ||
       (st = check_ints("free_list", free_list)) || (st = check_ints("pool", pool)) ||
       (st = check_ints("len_out", len_out)) || (st = check_ints("q_start", q_start)) ||
@@ -193,7 +200,7 @@ uc_status uc_page_attend(const uc_page_cache* cache, int Hq, const void* q, uc_d
 }
 
 size_t uc_beam_select_workspace_size(int R, int W, int V) {
-  if (R < 1 || W < 1 || W > UC_MAX_BEAMS || V < W || (int64_t)W * V > INT32_MAX || (int64_t)R * W > (1 << 23)) return 0;
+  if (R < 1 || W < 1 || W > UC_MAX_BEAMS || V < W || (int64_t)W * V > kMostIndex || (int64_t)R * W > (1 << 23)) return 0;
   return beam_select_workspace(R, W, V);
 }
 
@@ -202,7 +209,7 @@ uc_status uc_beam_select(int R, int W, int V, const void* logits, uc_dtype dt, i
                          uint8_t* done_out, void* ws, size_t ws_bytes, void* stream) {
   if (R < 1 || W < 1 || W > UC_MAX_BEAMS)
     return fail(UC_E_INVALID, "R %d must be >= 1 and W %d in [1,%d]", R, W, UC_MAX_BEAMS);
-  if (V < W || (int64_t)W * V > INT32_MAX) return fail(UC_E_INVALID, "V %d must be at least W, W * V < 2^31", V);
+  if (V < W || (int64_t)W * V > kMostIndex) return fail(UC_E_INVALID, "V %d must be at least W, W * V <= 2^30", V);
   if ((int64_t)R * W > (1 << 23)) return fail(UC_E_UNSUPPORTED, "more than 2^23 beams");
   if (!dtype_ok(dt)) return fail(UC_E_INVALID, "bad dtype %d", dt);
   if (!logits || ((uintptr_t)logits & (dt == UC_F32 ? 3u : 1u)))

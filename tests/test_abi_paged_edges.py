@@ -6,7 +6,7 @@ import pytest
 import torch
 
 import paper_2609_32831_amd as uc
-from test_abi_paged import ATTEND, L, call
+from test_abi_paged import ATTEND, FREE, SELECT, STEP, E, L, U, call
 
 
 def test_a_single_token_has_no_distance():
@@ -52,3 +52,16 @@ def test_a_failed_launch_leaves_the_last_kernel():
     t.start()
     t.join()
     assert got == [(uc.UC_E_DEVICE, ""), (uc.UC_E_DEVICE, "")]
+
+
+def test_limits_of_the_kernels_indexes():
+    """Sizes whose next stride passes 31 bits are refused, not launched."""
+    most = (1 << 31) - 1
+    for kw in (dict(S=most), dict(ld=most), dict(ld=(1 << 30) + 1)):
+        assert call(L.uc_page_free, FREE, **kw) == U and uc.uc_last_error(), kw
+    for kw in (dict(S=most), dict(ld=most), dict(n_slots=most), dict(n_slots=(1 << 30) + 1)):
+        assert call(L.uc_page_step, STEP, **kw) == U and uc.uc_last_error(), kw
+    for W, V in ((1, most), (1, (1 << 30) + 1), (2, (1 << 29) + 1)):
+        assert call(L.uc_beam_select, SELECT, W=W, V=V, ld=V) == E and uc.uc_last_error(), (W, V)
+        assert L.uc_beam_select_workspace_size(1, W, V) == 0
+    assert L.uc_beam_select_workspace_size(1, 2, 1 << 29) > 0
