@@ -685,8 +685,9 @@ uc_status uc_page_read(const uc_page_cache* cache, const int32_t* slots, int T, 
  *   o       [T, Hq, D] of q_dt, 16-byte aligned, not overlapping q
  *   lse     optional float [T, Hq]: natural-log log-sum-exp of the logits
  *   max_q   at least the largest n; a sequence with more tokens may be left out
- * Rows of any size may lie behind those that a query sees.  A query that sees
- * values above 2^88, or logits beyond binary32, may get infinities or NaN.
+ * Rows of any size may lie behind those that a query sees.  A query of elements
+ * above 2^100, or one that sees values above 2^88 or logits beyond binary32, may
+ * get infinities, NaN or zeros.
  * Tokens of no sequence keep their o and lse.  q_start and len are held to
  * [0, T] and the table's rows.  Rows of a sequence whose table names a page
  * outside the cache within its length may be NaN, and those that see it are.

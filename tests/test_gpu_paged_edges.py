@@ -39,6 +39,23 @@ def test_queries_of_one_sign(tokens, size, D, group, dtype):
     check_sized(cache, q, [0, tokens], lens, table, float(np.float32(0.1)), o, lse, dtype)
 
 
+@pytest.mark.parametrize("group", [32, 128])
+@pytest.mark.parametrize("tokens", [3, 70])
+def test_queries_as_large_as_they_may_be(tokens, group):
+    """Elements up to 2^100, of one sign and of both, over keys as small."""
+    _case(test="largest", tokens=tokens, group=group)
+    lens, Hkv, G, D = [150], 2, 2, 128
+    cache, table = make_cache(lens, 16, Hkv, D, group, 105)
+    r = np.random.default_rng(106)
+    put_rows(cache, table, 0, range(150), r.standard_normal((150, Hkv, D)) * 2.0 ** -99, r.standard_normal((150, Hkv, D)))
+    q = r.random((tokens, Hkv * G, D)) + 1
+    q[::2] *= r.choice([-1, 1], q[::2].shape)
+    q = torch.tensor(q * 2.0 ** 99, device="cuda").bfloat16()
+    o, lse = torch.empty_like(q), torch.empty(tokens, Hkv * G, device="cuda")
+    uc.uc_page_attend(cache.device(uc), q, i32([0, tokens]), i32(lens), i32(table), tokens, 0.1, o, lse)
+    check_sized(cache, q, [0, tokens], lens, table, float(np.float32(0.1)), o, lse, "bf16")
+
+
 @pytest.mark.parametrize("peak", [100, 61000])
 @pytest.mark.parametrize("tokens,G", [(3, 1), (4096, 16)])
 def test_a_long_tail_under_a_peak(tokens, G, peak):
@@ -76,6 +93,42 @@ def test_a_long_tail_under_a_peak(tokens, G, peak):
     bound = (half("f16") + 2.0 ** -12 + logit * D * 22 * 2.0 ** -24) * want + n * 2.0 ** -32
     assert np.all(err <= bound)
     assert np.all(np.abs(f64(lse) - want_lse) <= 1e-5 * want_lse + 2.0 ** -12)
+
+
+# ---------------------------------------------------------------- starts and lengths
+
+@pytest.mark.parametrize("path", ["auto", "valu"])
+@pytest.mark.parametrize("G", [2, 32])
+@pytest.mark.parametrize("start,lens,rows", [
+    ([-5, 3, 900], [64, 40], [64, 40]),
+    ([0, 5, 2], [10 ** 9, -4], [64, 0]),
+    ([1, 3, 6], [64, -7], [64, 0]),
+    ([6, 6, 6], [64, 64], [64, 64]),
+    ([900, -3, 4], [64, 64], [64, 64]),
+    ([2, 5, 3], [64, 64], [64, 64]),
+])
+def test_starts_and_lengths_are_held_to_the_arrays(start, lens, rows, G, path):
+    """A sequence's tokens and rows count as far as the arrays go; tokens of no
+    sequence keep what they have.  (32 heads a KV head: the prompt kernel.)"""
+    _case(test="held", start=start, lens=lens, G=G, path=path)
+    cache, table = make_cache([64, 64], 16, 1, 64, 32, 41)
+    q = torch.randn(6, G, 64, device="cuda", dtype=torch.bfloat16)
+    o, lse = torch.full_like(q, 5.0), torch.full((6, G), 5.0, device="cuda")
+    prev = uc.uc_set_path(uc.UC_PATH_VALU if path == "valu" else uc.UC_PATH_AUTO)
+    try:
+        uc.uc_page_attend(cache.device(uc), q, i32(start), i32(lens), i32(table), 6, 0.1, o, lse)
+        torch.cuda.synchronize()
+    finally:
+        uc.uc_set_path(prev)
+    want, want_lse = ref.attend(cache, f64(q), np.clip(start, 0, 6), rows, table, float(np.float32(0.1)))
+    none = np.isnan(want).all((1, 2))
+    assert torch.all(o[torch.from_numpy(none)] == 5.0) and torch.all(lse[torch.from_numpy(none)] == 5.0)
+    some = torch.from_numpy(~none)
+    got, got_lse, want, want_lse = f64(o[some]), f64(lse[some]), want[~none], want_lse[~none]
+    empty = np.isneginf(want_lse)
+    assert np.array_equal(empty, np.isneginf(got_lse)) and np.all(got[empty] == 0)
+    assert np.all(np.abs(got - want) <= 2e-3 + half("bf16") * np.abs(want))
+    assert np.allclose(got_lse[~empty], want_lse[~empty], rtol=1e-5, atol=1e-4)
 
 
 # ---------------------------------------------------------------- equal beams
