@@ -689,7 +689,8 @@ uc_status uc_page_read(const uc_page_cache* cache, const int32_t* slots, int T, 
  * above 2^100, or one that sees values above 2^88 or logits beyond binary32, may
  * get infinities, NaN or zeros.
  * Tokens of no sequence keep their o and lse.  q_start and len are held to
- * [0, T] and the table's rows.  Rows of a sequence whose table names a page
+ * [0, T] and the table's rows; tokens that several sequences claim get either's
+ * result, or keep theirs.  Rows of a sequence whose table names a page
  * outside the cache within its length may be NaN, and those that see it are.
  * Sequences with n * (Hq / Hkv) <= 64 and longer ones are taken by kernels of
  * their own in the same call ("page_tokens", "page_prompt" for

@@ -242,10 +242,11 @@ __device__ inline int prompt_tiles(const Seq& x, int G, int b) {
 }
 
 // before[s]: units of the sequences ahead of s, before[S]: all of them (by one
-// workgroup of 256)
-__device__ inline void plan_prompts(const PageAttendArgs& a, int* __restrict__ before, int* part) {
+// workgroup of 256).  Only starts by which sequences share tokens can give more
+// than the host allows for: then there are none, and no prompt is taken.
+__device__ inline void plan_prompts(const PageAttendArgs& a, int* __restrict__ before, int64_t* part) {
   const int lane = threadIdx.x & 63;
-  int base = 0;
+  int64_t base = 0;
   for (int s0 = 0; s0 < a.S; s0 += 256) {
     const int s = s0 + threadIdx.x;
     Seq x{0, 0, 0};
@@ -263,12 +264,12 @@ __device__ inline void plan_prompts(const PageAttendArgs& a, int* __restrict__ b
       for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
       if (lane == from) mine = sum;
     }
-    int total;
-    const int upto = block_scan(mine, part, total);
-    if (s < a.S) before[s] = base + upto - mine;
+    int64_t total;
+    const int64_t upto = block_scan((int64_t)mine, part, total);
+    if (s < a.S) before[s] = (int)(base + upto - mine);
     base += total;
   }
-  if (threadIdx.x == 0) before[a.S] = base;
+  if (threadIdx.x == 0) before[a.S] = base > INT32_MAX ? 0 : (int)base;
 }
 
 // ---------------------------------------------------------------- single tokens
@@ -349,7 +350,7 @@ __global__ __launch_bounds__(256, 2) void page_tokens_kernel(PageAttendArgs a, i
   const int G = a.G, Hq = G * Hkv, lgP = a.pc.lgP, P1 = (1 << lgP) - 1;
   const Magic magic;
   if ((int)(blockIdx.x / Hkv * (SOLO ? WAVES : 1)) == W_all) {  // one workgroup more where prompts follow: their plan
-    plan_prompts(a, units_out, reinterpret_cast<int*>(lds));
+    plan_prompts(a, units_out, reinterpret_cast<int64_t*>(lds));
     return;
   }
   const int turn = SOLO ? 0 : wave;  // the wave's among a piece's tiles
@@ -889,7 +890,6 @@ __global__ __launch_bounds__(64 * PWAVES, 2) void page_prompt_kernel(PageAttendA
   s = __builtin_amdgcn_readfirstlane(s);
   Seq x = scalar(seq_of(a, s));
   int nb = prompt_blocks(x, G);
-  if (threadIdx.x == 0) s_block = -1;
   {
     int base = units[s];
     for (int b0 = 0; b0 < nb; b0 += THREADS) {
@@ -909,7 +909,6 @@ __global__ __launch_bounds__(64 * PWAVES, 2) void page_prompt_kernel(PageAttendA
     (&keys[0].m[0][0])[i] = (&keys[1].m[0][0])[i] = (&keys[2].m[0][0])[i] = (_Float16)0.0f;
   __syncthreads();
   int b = __builtin_amdgcn_readfirstlane(s_block);
-  if (b < 0) return;  // starts that overlap so often that the sums passed their type
   int before = __builtin_amdgcn_readfirstlane(s_before);
 
   // A thread's share of a stage: 16 bytes of codes of a row, of keys (the

@@ -131,6 +131,24 @@ def test_starts_and_lengths_are_held_to_the_arrays(start, lens, rows, G, path):
     assert np.allclose(got_lse[~empty], want_lse[~empty], rtol=1e-5, atol=1e-4)
 
 
+def test_tokens_that_many_sequences_claim():
+    """800 sequences of the same 62500 tokens over 128000 rows hold more work
+    than a call's indexes count: no prompt is taken, and what was there stays.
+    The next call is an ordinary one."""
+    T, G, D, P, m = 62500, 16, 64, 1024, 800
+    cache = uc.page_cache(125, P, 1, D, 64)
+    for x in cache.t.values():
+        x.zero_()
+    start = i32([0, T] * m + [0])
+    lens, table = i32([128000] * (2 * m)), torch.arange(125, device="cuda", dtype=torch.int32).repeat(2 * m, 1)
+    q = torch.zeros(T, G, D, device="cuda", dtype=torch.bfloat16)
+    o = torch.full_like(q, 5.0)
+    uc.uc_page_attend(cache, q, start, lens, table, T, 0.1, o)
+    assert torch.all(o == 5.0)
+    uc.uc_page_attend(cache, q[:300], i32([0, 300]), lens[:1], table[:1], 300, 0.1, o[:300])
+    assert torch.all(o[:300] == 0) and torch.all(o[300:] == 5.0)
+
+
 # ---------------------------------------------------------------- equal beams
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
