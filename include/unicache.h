@@ -610,7 +610,8 @@ size_t uc_attend_batch_workspace_size(const uc_shape* shape,
  * to 4 significant bits (so that c * s is a bf16 exactly); code = s > 0 ?
  * clamp(rint((x - m) / s), 0, 15) : 0.  Before that every x is held to
  * +-2^126 and a NaN becomes 0, so a cache written by uc_page_append holds
- * finite values only.
+ * finite values only.  (m is to the nearest: that of bf16 rows is exact; a group
+ * of other rows that spreads by less than 2^-8 of its offset keeps little of it.)
  * D is 64 or 128; group 32, 64 or 128 and at most D; page_rows a power of two
  * in [16, 1024]; n_pages * page_rows < 2^31; pointers 16-byte aligned. */
 typedef struct {

@@ -9,11 +9,16 @@
 // the elements that pass a floor, which W elements are known to reach, and
 // raises the floor when its list is full; so an element costs a multiply-add,
 // an exponential, an addition and its share of a comparison.  384 rows of
-// 131071 bf16 (87 MB without the beams that ended): 28 us, 3.1 TB/s.  (W best
-// kept in order in the wave's lanes instead: 49 us.)  The choice among the
-// candidates takes 8 us, most of it W dependent steps over a wave.  A whole
-// selection of 384 live rows: 35 us, 43 where a mask leaves one logit in a
-// thousand, 700 where rows rise all along.
+// 131071 bf16, of which 308 are live (81 MB): 29 us, 2.8 TB/s.  (W best kept in
+// order in the wave's lanes instead: 49 us.)  The choice among the candidates
+// takes 8 us, most of it W dependent steps over a wave.  A whole selection of
+// 384 live rows: 36 us, 44 where a mask leaves one logit in a thousand, 705 where
+// rows rise all along.
+//
+// The first floor stands once each of the four waves has W / 4 vectors.  Shorter
+// rows (below some 1550 elements of 16 bits, half of that in binary32) are
+// gathered whole and ranked by comparing all pairs, which costs more than a long
+// row: 384 rows of 300, 1000 and 1500 bf16 take 24, 83 and 170 us, of 2000 14.
 //
 // Reordering.  A beam's pages before the one being filled are full and may be
 // shared; that last page is each beam's own.  The first child of a beam keeps
@@ -590,8 +595,8 @@ __global__ __launch_bounds__(256) void beam_reorder_kernel(ReorderArgs a) {
 }
 
 // Splits of a row: six workgroups per CU over all rows at most, which run in one
-// round (384 rows of 131071 in two, three, four and six splits: 43.8, 43.0, 38.8
-// and 41.9 us a step with its reordering), a span of at least 2048 elements (a workgroup's
+// round (384 rows of 131071 in two, three, four and six splits: 45.1, 45.9, 39.6
+// and 43.7 us a step with its reordering), a span of at least 2048 elements (a workgroup's
 // fixed work is a few microseconds), and candidates that the second kernel
 // holds in registers.
 int beam_splits(int R, int W, int V) {

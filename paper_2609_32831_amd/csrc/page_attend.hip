@@ -757,12 +757,11 @@ __global__ __launch_bounds__(256, 2) void page_tokens_kernel(PageAttendArgs a, i
 // largest weight at 2^7 .. 2^15, so that the small ones of a long tail are fp16's
 // too: what lies below its subnormal step is off by 2^-32 of the largest (with
 // the largest at 1, a tail of 65500 keys of 2^-25.5 each, a 700th of the sum, was
-// lost from o and not from l).  The minima go through matrix
-// instructions of their own, q . k += sum_g m_g sum(q_g) with sum(q_g) in
-// three fp16 parts.  Queries enter as fp16 too, a row far from 1, or of sums
-// that fp16 does not hold, by a power of two: as such a row stands, its elements
-// below 2^-14 are off by 2^-25 at most, 2^-21 of its largest; the others are
-// exact.
+// lost from o and not from l; 1 % faster).  The minima go through matrix
+// instructions of their own, q . k += sum_g m_g sum(q_g) with sum(q_g) in three
+// fp16 parts.  Queries enter as fp16 too, a row far from 1, or of sums that fp16
+// does not hold, by a power of two: as such a row stands, its elements below
+// 2^-14 are off by 2^-25 at most, 2^-21 of its largest; the others are exact.
 //
 // Rows of more different sizes within 16 (one of infinities, say, that earlier
 // queries do not see), values beyond 2^-60 .. 2^76 and logits beyond 2^16 mark
@@ -771,13 +770,14 @@ __global__ __launch_bounds__(256, 2) void page_tokens_kernel(PageAttendArgs a, i
 // for them costs 2 % of the kernel's time.
 //
 // Four prompts of 1500 tokens over up to 8192 rows, 28 query heads on 4, D 128
-// (342 GFLOP): 460 us a call, 745 TFLOP/s.  A stage of 64 keys x 32 rows is 76
+// (342 GFLOP): 465 us a call, 736 TFLOP/s.  A stage of 64 keys x 32 rows is 76
 // matrix instructions a wave and five vector instructions to each of those,
 // most of them for the softmax; the two do not overlap fully with the two waves
 // a SIMD holds.  Tried: four waves a workgroup, each tile then staged for half
 // the rows (709 us); two buffers and a barrier per tile instead of the
 // pipeline of steps (530 us); bf16 planes (578 us); fixed orders of matrix and
 // vector instructions (498 to 553 us) - the compiler's own is the best.
+
 // A raised reference puts the largest weight at 2^kPeak; it is raised once a
 // weight passes 2^kRaise, which is looked at where the eight weights of a lane
 // together pass kTop = 8 * 2^kRaise, the last power that fp16 holds.

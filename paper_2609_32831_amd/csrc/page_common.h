@@ -4,8 +4,9 @@
 // A row (one KV head of one token, D channels) is D/2 bytes of 4-bit codes and
 // NG = D / group scale words.  A word holds the group's step s (low half, a
 // bf16 with 4 significant bits) and minimum m (high half, a bf16); a code c
-// stands for c * s + m.  c has 4 significant bits and s has 4, so c * s is a
-// bf16 exactly: the prompt kernel's matrix products take it in one plane.
+// stands for c * s + m.  c has 4 significant bits and s has 4, so c * s has 8: the
+// prompt kernel's matrix products take it in one plane, in fp16 with a power of
+// two of 16 rows taken out; the single-token kernel's take c.
 // Keys' codes lie in the order of the matrix operand (16 keys x 32 channels,
 // lane (key, g) holding 8 channels of every 32): the 32-bit word (D/32) g + t
 // of a row holds channels 32 t + 8 g .. 32 t + 8 g + 7, so that a lane's codes

@@ -12,10 +12,11 @@
 // Bound by bytes: 2 D elements in and D + 8 NG bytes out per row and head.
 // 16 lanes (D = 128) or 8 (D = 64) take a row's keys and values, 8 channels of
 // each: one 16-byte load of 16-bit rows, one 4-byte store of codes.  16001 rows
-// of 4 heads of 128 bf16 (42 MB): append 14.1 us, read 8.7 us.  The append is
-// still held up by its arithmetic, some 11 instructions an element (with true
-// divisions 18.6 us; keys and values by different threads 16.4; every element
-// held to its bounds 15.6).
+// of 4 heads of 128 bf16 (42 MB): append 14 us, read 9 us.  The append is held up
+// by its arithmetic, 25 vector instructions an element (406 a wave for 16 elements
+// a lane: two divisions, a reciprocal, the bounds and the steps between lanes
+// among them; with a division for every element 18.6 us; keys and values by
+// different threads 16.4; every element held to its bounds 15.6).
 #include "page_common.h"
 
 namespace uc {
